@@ -427,6 +427,74 @@ fv_status fv_generate(fv_ctx *ctx, const fv_generator *gen, const float *start_d
                       float *r_out_dev, void *workspace_dev, size_t workspace_bytes, void *stream);
 
 /* ------------------------------------------------------------------------------------------------
+ * (5) What the rows of logits say (no counterpart in the paper, which reports image quality alone): how likely given tokens
+ *     are, how sure a row is, which tokens came next; and how far a pruned schedule's rows are from the unpruned
+ *     one's, as a loss over the unpruned one's top logits with its gradient.  For a row x of V logits at temperature tau
+ *         m = max_j x_j,   L = ln sum_j exp((x_j - m) / tau),   p_j = exp((x_j - m) / tau - L).
+ *   logits_dev  [rows, V] of dtype 0: fp32, 1: bf16; row r starts ld elements (ld >= V) after row r - 1.  Rows may start at any
+ *               address of their type and V may be odd.  V * (size of an element) <= 1.5 MiB, else UNSUPPORTED.
+ *   tau         1e-6 ... 1e6.
+ *   stats       [rows] pairs (m, L), 8-byte aligned: what the gradient calls take.  ln sum_j exp(x_j / tau) = m / tau + L.
+ *   Logits of -inf have p = 0.  A row of nothing but -inf has p = 0 everywhere: m = L = logprob = -inf, entropy 0, gradient 0.
+ *   A row that holds a NaN or +inf: every result of it is NaN (m: the largest of the others), its alternatives -1.
+ *   A row whose gradient's weights are all 0, or that has no token, has gradient 0 whatever its logits are.
+ *   Token ids: -1 stands for none; another id outside [0, V) sets *status_dev (int32 device word, or NULL) to 40, makes the row's
+ *   log probability or loss NaN and counts as none in the gradients.
+ *   dlogits_out_dev [rows, V] of the type of the logits, rows ld_out elements apart, rounded once from fp32; it may be logits_dev itself (with
+ *               ld_out = ld) and must not overlap it otherwise.  Fastest where both rows start at the same offset from a 16-byte boundary.
+ *   Outputs other than these rows (what lies between V and ld) are left as they are.  Sums and statistics are fp32, every result
+ *   is the same bits run to run, and no call needs a workspace unless it says so. */
+
+/* Log probabilities of given tokens, entropy, alternatives.
+ *   ids_dev [rows] int32 and logprob_out_dev [rows] fp32, or both NULL: ln p of the row's token; 0 where the id is -1.
+ *   stats_out_dev, entropy_out_dev [rows] (-sum_j p_j ln p_j): fp32 or NULL.
+ *   n_alt 0 ... 64: alt_ids_out_dev int32, alt_logprob_out_dev fp32, both [rows, n_alt]: the n_alt largest logits in descending order, the
+ *               lowest id first among equals (-0 equals 0), and their ln p.  -inf is no alternative: id -1, -inf fill the rest.
+ * Errors: INVALID_ARG, UNSUPPORTED, CUDA. */
+fv_status fv_token_logprobs(const void *logits_dev, int32_t dtype, int64_t ld, int32_t rows, int32_t V, float tau,
+                            const int32_t *ids_dev, int32_t n_alt, float *logprob_out_dev, float *stats_out_dev,
+                            float *entropy_out_dev, int32_t *alt_ids_out_dev, float *alt_logprob_out_dev,
+                            int32_t *status_dev, void *stream);
+/* dlogits = g_logprob * d logprob / d logits + g_entropy * d entropy / d logits, for weights per row:
+ *   (1[j = id] - p_j) g_logprob / tau - p_j (ln p_j + entropy) g_entropy / tau.
+ *   stats_dev, entropy_dev: what fv_token_logprobs gave for these logits; entropy_dev is needed with g_entropy_dev only.
+ *   ids_dev goes with g_logprob_dev, either pair may be NULL, not both. */
+fv_status fv_token_logprobs_grad(const void *logits_dev, int32_t dtype, int64_t ld, int32_t rows, int32_t V, float tau,
+                                 const int32_t *ids_dev, const float *stats_dev, const float *entropy_dev,
+                                 const float *g_logprob_dev, const float *g_entropy_dev, void *dlogits_out_dev,
+                                 int64_t ld_out, int32_t *status_dev, void *stream);
+
+/* Distillation from a teacher's top logits: loss[r] = sum_k q_k (ln q_k - ln p_{id_k}), q = softmax(teacher_logits / tau) over the row's
+ * K entries, p over the whole row of logits.
+ *   teacher_ids_dev int32, teacher_logits_dev fp32, both [rows, K], K 1 ... 128; log probabilities do as well as logits (the
+ *               alternatives of fv_token_logprobs on the teacher's rows).  Entries with id -1 or a logit of -inf are left out; a row
+ *               without entries has loss 0.  An id may come more than once; its entries add up.
+ *   loss_out_dev [rows] fp32; stats_out_dev or NULL.
+ *   dlogits_out_dev NULL, or the gradient in the same pass: g_loss[r] (p_j - sum_{k: id_k = j} q_k) / tau, g_loss_dev [rows] fp32 or NULL (1);
+ *               g_loss_dev is NULL without dlogits_out_dev.
+ * Errors: INVALID_ARG, UNSUPPORTED, CUDA. */
+fv_status fv_distill_topk(const void *logits_dev, int32_t dtype, int64_t ld, int32_t rows, int32_t V, float tau,
+                          const int32_t *teacher_ids_dev, const float *teacher_logits_dev, int32_t K,
+                          const float *g_loss_dev, float *loss_out_dev, float *stats_out_dev, void *dlogits_out_dev,
+                          int64_t ld_out, int32_t *status_dev, void *stream);
+/* The gradient alone, for weights that are known after the loss; stats_dev as fv_distill_topk left them. */
+fv_status fv_distill_topk_grad(const void *logits_dev, int32_t dtype, int64_t ld, int32_t rows, int32_t V, float tau,
+                               const int32_t *teacher_ids_dev, const float *teacher_logits_dev, int32_t K,
+                               const float *stats_dev, const float *g_loss_dev, void *dlogits_out_dev, int64_t ld_out,
+                               int32_t *status_dev, void *stream);
+
+/* Log probabilities of given tokens, statistics and entropy (as fv_token_logprobs) of the rows a * W^T + bias, which are not kept:
+ * the likelihood of a token map under the output head.
+ *   a_dev bf16 [rows, C] (fv_gather_ln's output for the head), w_dev bf16 [V, C], bias_dev bf16 [V] or NULL; C % 8 == 0, V % 8 == 0, all
+ *   16-byte aligned, as for fv_gemm_bf16 (W is a constant of the stream).  Products accumulate in fp32; logits stay fp32.
+ *   workspace_dev: fv_linear_logprobs_workspace_bytes(rows, V) bytes, 256-byte aligned.  Errors: INVALID_ARG, UNSUPPORTED, CAPACITY, CUDA. */
+size_t fv_linear_logprobs_workspace_bytes(int32_t rows, int32_t V);
+fv_status fv_linear_logprobs(const void *a_dev, const void *w_dev, const void *bias_dev, int32_t rows, int32_t C, int32_t V,
+                             float tau, const int32_t *ids_dev, float *logprob_out_dev, float *stats_out_dev,
+                             float *entropy_out_dev, void *workspace_dev, size_t workspace_bytes, int32_t *status_dev,
+                             void *stream);
+
+/* ------------------------------------------------------------------------------------------------
  * Measurement support (no counterpart in the paper; Appendix "efficiency profiling" motivates the
  * per-module breakdown).  Kernel classes, in array order: 0 select (column mean + score + top-k),
  * 1 gather+LayerNorm, 2 GEMM, 3 attention, 4 restore.

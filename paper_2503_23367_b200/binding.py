@@ -27,7 +27,9 @@ EXPORTS = ["fv_status_string", "fv_k_for", "fv_prune_select_workspace_bytes", "f
            "fv_kernel_launches", "fv_profile_enable", "fv_profile_read",
            "fv_prune_select_static", "fv_prune_select_static_capacity",
            "fv_head_workspace_bytes", "fv_head_tokens", "fv_argmax_rows", "fv_residual_accumulate", "fv_next_scale_input",
-           "fv_generate_workspace_bytes", "fv_generate", "fv_var_step_host_staging_bytes", "fv_var_step_host", "fv_host_io_flush", "fv_struct_sizes"]
+           "fv_generate_workspace_bytes", "fv_generate", "fv_var_step_host_staging_bytes", "fv_var_step_host", "fv_host_io_flush", "fv_struct_sizes",
+           "fv_token_logprobs", "fv_token_logprobs_grad", "fv_distill_topk", "fv_distill_topk_grad",
+           "fv_linear_logprobs_workspace_bytes", "fv_linear_logprobs"]
 
 
 class FvError(RuntimeError):
@@ -120,6 +122,18 @@ def lib() -> C.CDLL:
         L.fv_generate_workspace_bytes.restype = sz; L.fv_generate_workspace_bytes.argtypes = [vp, C.POINTER(fv_generator)]
         L.fv_generate.restype = C.c_int
         L.fv_generate.argtypes = [vp, C.POINTER(fv_generator), vp, i32, C.POINTER(dbl), C.POINTER(vp), vp, vp, vp, sz, vp]
+        i64 = C.c_int64
+        L.fv_token_logprobs.restype = C.c_int
+        L.fv_token_logprobs.argtypes = [vp, i32, i64, i32, i32, f32, vp, i32, vp, vp, vp, vp, vp, vp, vp]
+        L.fv_token_logprobs_grad.restype = C.c_int
+        L.fv_token_logprobs_grad.argtypes = [vp, i32, i64, i32, i32, f32, vp, vp, vp, vp, vp, vp, i64, vp, vp]
+        L.fv_distill_topk.restype = C.c_int
+        L.fv_distill_topk.argtypes = [vp, i32, i64, i32, i32, f32, vp, vp, i32, vp, vp, vp, vp, i64, vp, vp]
+        L.fv_distill_topk_grad.restype = C.c_int
+        L.fv_distill_topk_grad.argtypes = [vp, i32, i64, i32, i32, f32, vp, vp, i32, vp, vp, vp, i64, vp, vp]
+        L.fv_linear_logprobs_workspace_bytes.restype = sz; L.fv_linear_logprobs_workspace_bytes.argtypes = [i32, i32]
+        L.fv_linear_logprobs.restype = C.c_int
+        L.fv_linear_logprobs.argtypes = [vp, vp, vp, i32, i32, i32, f32, vp, vp, vp, vp, vp, sz, vp, vp]
         L.fv_var_step_host_staging_bytes.restype = sz; L.fv_var_step_host_staging_bytes.argtypes = [C.POINTER(fv_config)]
         L.fv_var_step_host.restype = C.c_int; L.fv_var_step_host.argtypes = [vp, vp, i32, i32, dbl, vp, vp, sz, vp]
         L.fv_host_io_flush.restype = C.c_int; L.fv_host_io_flush.argtypes = [vp, vp]
@@ -356,6 +370,119 @@ def fv_next_scale_input(r: torch.Tensor, h: int, w: int, h2: int, w2: int, w_in:
     _check(lib().fv_next_scale_input(_ptr(r), B, h, w, d, h2, w2, _ptr(w_in), _ptr(b_in), _ptr(pos), Cw, _ptr(out), _stream()),
            "fv_next_scale_input")
     return out
+
+
+def _rows(logits: torch.Tensor):
+    """(address, dtype code, row stride, rows, V) of a 2-D tensor of logits whose rows are contiguous, on the current device."""
+    assert logits.is_cuda and logits.dim() == 2 and (logits.stride(1) == 1 or logits.shape[1] == 1), "logits are [rows, V] CUDA tensors with contiguous rows"
+    assert logits.device.index == torch._C._cuda_getDevice(), "the logits are on another device than the current one"
+    dtype = logits.dtype
+    assert dtype == torch.float32 or dtype == torch.bfloat16, "logits are float32 or bfloat16"
+    rows, V = logits.shape
+    return logits.data_ptr(), 1 if dtype == torch.bfloat16 else 0, logits.stride(0) if rows > 1 else V, rows, V
+
+
+def _arg(t: Optional[torch.Tensor], dtype: torch.dtype, shape, like: torch.Tensor) -> Optional[int]:
+    """Address of a contiguous tensor of that type and shape on the logits' device, or None."""
+    if t is None:
+        return None
+    assert t.dtype == dtype and tuple(t.shape) == shape and t.device == like.device, f"expected {dtype} {list(shape)} on {like.device}"
+    return _ptr(t)
+
+
+def _grad_out(logits: torch.Tensor, out: Optional[torch.Tensor]):
+    """The tensor of a gradient of the logits: given, or new with the logits' row stride (rows then start at the same offset from 16 bytes)."""
+    if out is None:
+        rows, V = logits.shape
+        ld = max(V, logits.stride(0)) if rows > 1 else V
+        pad = (logits.data_ptr() & 15) // logits.element_size()
+        out = _empty((pad + rows * ld,), logits.dtype, logits.device).as_strided((rows, V), (ld, 1), pad)
+    assert out.dtype == logits.dtype and out.shape == logits.shape and out.device == logits.device and (out.stride(1) == 1 or out.shape[1] == 1)
+    return out, out.data_ptr(), out.stride(0) if out.shape[0] > 1 else out.shape[1]
+
+
+def fv_token_logprobs(logits: torch.Tensor, ids: Optional[torch.Tensor] = None, tau: float = 1.0, n_alt: int = 0,
+                      want_entropy: bool = False, status: Optional[torch.Tensor] = None) -> dict:
+    """logits [rows, V] fp32 or bf16 -> {"stats" [rows, 2] (m, L), "logprob" [rows] of ids (int32, -1 = none), "entropy" [rows],
+    "alt_ids" int32 / "alt_logprob" [rows, n_alt]}, the last three where asked for."""
+    x, dt, ld, rows, V = _rows(logits)
+    dev = logits.device
+    r = {"stats": _empty((rows, 2), torch.float32, dev)}
+    idp = _arg(ids, torch.int32, (rows,), logits)
+    if ids is not None:
+        r["logprob"] = _empty((rows,), torch.float32, dev)
+    if want_entropy:
+        r["entropy"] = _empty((rows,), torch.float32, dev)
+    if n_alt:
+        r["alt_ids"] = _empty((rows, max(n_alt, 0)), torch.int32, dev)
+        r["alt_logprob"] = _empty((rows, max(n_alt, 0)), torch.float32, dev)
+    at = lambda k: r[k].data_ptr() if k in r else None
+    _check(lib().fv_token_logprobs(x, dt, ld, rows, V, tau, idp, n_alt, at("logprob"), at("stats"), at("entropy"), at("alt_ids"),
+                                   at("alt_logprob"), _ptr(status), _stream()), "fv_token_logprobs")
+    return r
+
+
+def fv_token_logprobs_grad(logits: torch.Tensor, ids: Optional[torch.Tensor], stats: torch.Tensor, g_logprob: Optional[torch.Tensor],
+                           tau: float = 1.0, entropy: Optional[torch.Tensor] = None, g_entropy: Optional[torch.Tensor] = None,
+                           out: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Gradient of sum_r g_logprob[r] logprob[r] + g_entropy[r] entropy[r] by the logits; out may be the logits themselves."""
+    x, dt, ld, rows, V = _rows(logits)
+    out, op, ldo = _grad_out(logits, out)
+    f32 = torch.float32
+    _check(lib().fv_token_logprobs_grad(x, dt, ld, rows, V, tau, _arg(ids, torch.int32, (rows,), logits), _arg(stats, f32, (rows, 2), logits),
+                                        _arg(entropy, f32, (rows,), logits), _arg(g_logprob, f32, (rows,), logits),
+                                        _arg(g_entropy, f32, (rows,), logits), op, ldo, _ptr(status), _stream()), "fv_token_logprobs_grad")
+    return out
+
+
+def fv_distill_topk(logits: torch.Tensor, teacher_ids: torch.Tensor, teacher_logits: torch.Tensor, tau: float = 1.0,
+                    g_loss: Optional[torch.Tensor] = None, want_grad: bool = False, out: Optional[torch.Tensor] = None,
+                    status: Optional[torch.Tensor] = None) -> dict:
+    """Loss per row against a teacher's top logits ([rows, K], ids int32, -1 = no entry): {"loss" [rows], "stats" [rows, 2]} and, with
+    want_grad, "dlogits" = g_loss[r] * its gradient (g_loss None: 1) from the same pass; out may be the logits themselves."""
+    x, dt, ld, rows, V = _rows(logits)
+    K = teacher_ids.shape[-1]
+    dev, f32 = logits.device, torch.float32
+    r = {"loss": _empty((rows,), f32, dev), "stats": _empty((rows, 2), f32, dev)}
+    op, ldo = None, 0
+    if want_grad:
+        r["dlogits"], op, ldo = _grad_out(logits, out)
+    _check(lib().fv_distill_topk(x, dt, ld, rows, V, tau, _arg(teacher_ids, torch.int32, (rows, K), logits), _arg(teacher_logits, f32, (rows, K), logits), K,
+                                 _arg(g_loss, f32, (rows,), logits), r["loss"].data_ptr(), r["stats"].data_ptr(), op, ldo, _ptr(status), _stream()), "fv_distill_topk")
+    return r
+
+
+def fv_distill_topk_grad(logits: torch.Tensor, teacher_ids: torch.Tensor, teacher_logits: torch.Tensor, stats: torch.Tensor,
+                         g_loss: Optional[torch.Tensor] = None, tau: float = 1.0, out: Optional[torch.Tensor] = None,
+                         status: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """g_loss[r] * gradient of fv_distill_topk's loss by the logits, from the stats it left; out may be the logits themselves."""
+    x, dt, ld, rows, V = _rows(logits)
+    K = teacher_ids.shape[-1]
+    out, op, ldo = _grad_out(logits, out)
+    f32 = torch.float32
+    _check(lib().fv_distill_topk_grad(x, dt, ld, rows, V, tau, _arg(teacher_ids, torch.int32, (rows, K), logits), _arg(teacher_logits, f32, (rows, K), logits), K,
+                                      _arg(stats, f32, (rows, 2), logits), _arg(g_loss, f32, (rows,), logits), op, ldo, _ptr(status), _stream()), "fv_distill_topk_grad")
+    return out
+
+
+def fv_linear_logprobs(a: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Tensor], ids: Optional[torch.Tensor] = None, tau: float = 1.0,
+                       want_entropy: bool = False, status: Optional[torch.Tensor] = None) -> dict:
+    """As fv_token_logprobs on the rows a [rows, C] * w [V, C]^T + bias [V] (all bf16), whose logits are not kept."""
+    rows, Cw = a.shape
+    V = w.shape[0]
+    assert a.dtype == torch.bfloat16 and a.is_cuda and a.device.index == torch._C._cuda_getDevice()
+    bf, dev, f32 = torch.bfloat16, a.device, torch.float32
+    ws_bytes = lib().fv_linear_logprobs_workspace_bytes(rows, V)
+    ws = _empty((ws_bytes + 256,), torch.uint8, dev)
+    r = {"stats": _empty((rows, 2), f32, dev)}
+    if ids is not None:
+        r["logprob"] = _empty((rows,), f32, dev)
+    if want_entropy:
+        r["entropy"] = _empty((rows,), f32, dev)
+    at = lambda k: r[k].data_ptr() if k in r else None
+    _check(lib().fv_linear_logprobs(_ptr(a), _arg(w, bf, (V, Cw), a), _arg(bias, bf, (V,), a), rows, Cw, V, tau, _arg(ids, torch.int32, (rows,), a),
+                                    at("logprob"), at("stats"), at("entropy"), (ws.data_ptr() + 255) // 256 * 256, ws_bytes, _ptr(status), _stream()), "fv_linear_logprobs")
+    return r
 
 
 class FvGenerator:
