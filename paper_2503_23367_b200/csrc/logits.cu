@@ -15,6 +15,8 @@
 #include <cfloat>
 #include <climits>
 #include <cstdint>
+#include <cstdlib>
+#include <type_traits>
 
 #include "internal.h"
 #include "sm100.cuh"   // the device status codes, cluster barriers
@@ -54,24 +56,19 @@ __device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
   asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
   return r;
 }
-__device__ __forceinline__ float warp_max(float v) {   // NaN counts as absent
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xFFFFFFFFu, v, o));
-  return v;
+__device__ __forceinline__ float warp_max(float v) {   // (no NaN comes here)
+  float r;
+  asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
+  return r;
 }
 __device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
   return v;
 }
-__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
-}
-__device__ __forceinline__ void cp_async_wait_all() { asm volatile("cp.async.wait_all;" ::: "memory"); }
-__device__ __forceinline__ uint32_t cluster_nctas() {
-  uint32_t r;
-  asm volatile("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(r));
-  return r;
+// Untiled copy global -> this CTA's shared memory, its bytes counted on `bar`.  Both addresses and the size are multiples of 16.
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint64_t* bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(smem_u32(bar)) : "memory");
 }
 __device__ __forceinline__ uint32_t peer_smem(const void* p, uint32_t cta) {   // the same shared-memory address in another CTA of the cluster
   uint32_t r;
@@ -108,14 +105,6 @@ template <> struct Elem<float> {
     }
     __device__ __forceinline__ float value() const { return m; }
   };
-  // whether a vector has an element of at least the threshold
-  struct AtLeast {
-    float t;
-    __device__ __forceinline__ explicit AtLeast(float thr) : t(thr) {}
-    __device__ __forceinline__ bool any(const uint4& u) const {
-      return fmaxf(fmaxf(__uint_as_float(u.x), __uint_as_float(u.y)), fmaxf(__uint_as_float(u.z), __uint_as_float(u.w))) >= t;
-    }
-  };
   static constexpr float kLowest = -FLT_MAX;
 };
 template <> struct Elem<__nv_bfloat16> {
@@ -148,11 +137,6 @@ template <> struct Elem<__nv_bfloat16> {
     __device__ __forceinline__ void add(const uint4& u) { m = __hmax2(m, max4(u)); }
     __device__ __forceinline__ float value() const { return fmaxf(__low2float(m), __high2float(m)); }
   };
-  struct AtLeast {
-    __nv_bfloat162 t;
-    __device__ __forceinline__ explicit AtLeast(float thr) : t(__float2bfloat162_rn(thr)) {}   // exact: thr is one of the row's values, or kLowest
-    __device__ __forceinline__ bool any(const uint4& u) const { return !__hblt2(max4(u), t); }
-  };
   static constexpr float kLowest = -3.3895313892515355e38f;
 };
 
@@ -171,39 +155,54 @@ __device__ __forceinline__ int alt_index(uint64_t key) { return (int)(0xFFFFFFFF
 
 // ---- the part of a row that a group of G threads holds in shared memory ---------------------------------------------------
 // Vectors of 16 bytes counted from the row's start rounded down to 16 bytes, so a row may start anywhere; elements of the first and last
-// vector that are not the row's are -inf, which no pass notices.  The cluster's CTAs split the vectors evenly.  Thread t holds the
-// vectors t, t + G, ... of its part; it alone copies, builds and reads them, so a row needs no barrier before it is used.
+// vector that are not the row's are -inf, which no pass notices.  The cluster's CTAs split the vectors evenly.  Thread t reads the
+// vectors t, t + G, ... of its part.
 template <typename T, int G> struct Slice {
   static constexpr int E = Elem<T>::E;
   const T* row;      // first logit of the row
   int off, V;        // elements between the 16-byte boundary and the row; logits of the row
   int v0, n, t;      // first vector of this part, their number; thread of the group
+  int head, tail;    // this part's vectors that hold elements in front of or behind the row, or -1
   uint4* s;          // [n]
-  __device__ __forceinline__ Slice(const T* row_, int V_, int rank, int parts, int t_, uint4* s_) : row(row_), V(V_), t(t_), s(s_) {
+  __device__ __forceinline__ Slice(const T* row_, int V_, int rank, int lg_parts, int t_, uint4* s_) : row(row_), V(V_), t(t_), s(s_) {
     off = (int)((reinterpret_cast<uintptr_t>(row) & 15u) / sizeof(T));
-    const int nv = (off + V + E - 1) / E, base = nv / parts, rem = nv - base * parts;
+    const int nv = (off + V + E - 1) / E, base = nv >> lg_parts, rem = nv & ((1 << lg_parts) - 1);
     n = base + (rank < rem);
     v0 = rank * base + min(rank, rem);
+    head = v0 == 0 && off > 0 ? 0 : -1;
+    tail = v0 + n == nv && (off + V) % E ? n - 1 : -1;
   }
   __device__ __forceinline__ int first_index(int v) const { return (v0 + v) * E - off; }   // index in the row of the vector's first element
-  __device__ __forceinline__ bool whole(int v) const { const int i = first_index(v); return i >= 0 && i + E <= V; }
+  __device__ __forceinline__ bool whole(int v) const { return v != head && v != tail; }
   __device__ __forceinline__ void build(int v) {
     T* d = reinterpret_cast<T*>(s + v);
     const int i0 = first_index(v);
+    float x[E];
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-      const bool in = i0 + e >= 0 && i0 + e < V;
-      Elem<T>::store(d + e, in ? Elem<T>::load(row + i0 + e) : -INFINITY);
-    }
+    for (int e = 0; e < E; ++e) x[e] = Elem<T>::load(row + min(max(i0 + e, 0), V - 1));   // all on their way before the first is stored
+#pragma unroll
+    for (int e = 0; e < E; ++e) Elem<T>::store(d + e, i0 + e >= 0 && i0 + e < V ? x[e] : -INFINITY);
   }
-  __device__ __forceinline__ void fetch() {
-    const char* g = reinterpret_cast<const char*>(row - off) + (size_t)v0 * 16;
-    const uint32_t d = smem_u32(s);
-    for (int v = t; v < n; v += G)
-      if (whole(v)) cp_async16(d + v * 16, g + (size_t)v * 16);
-    // the partial vectors: the row's first and last, where this part has them
-    if (t == 0 && n > 0 && !whole(0)) build(0);
-    if (n > 1 && (n - 1) % G == t && !whole(n - 1)) build(n - 1);
+  // One copy for all whole vectors, completed on `bar`; the partial ones are built by the threads that hold them.
+  __device__ __forceinline__ void fetch(uint64_t* bar) {
+    if (t == 0) {
+      const int lo = head == 0, hi = tail >= 0 ? max(n - 1, lo) : n;
+      const uint32_t bytes = (uint32_t)(hi - lo) * 16;
+      mbar_expect_tx(bar, bytes);
+      if (bytes) bulk_load(smem_u32(s + lo), reinterpret_cast<const char*>(row - off) + (size_t)(v0 + lo) * 16, bytes, bar);
+    }
+    if (t == 0 && head == 0) build(0);
+    if (tail >= 0 && tail != head && tail % G == t) build(tail);
+  }
+  // f(vector) for the thread's vectors, four loads at a time.
+  template <typename F> __device__ __forceinline__ void each(F f) const {
+    const uint4* q = s + t;
+    int left = n - t;
+    for (; left > 3 * G; left -= 4 * G, q += 4 * G) {
+      const uint4 a = q[0], b = q[G], c = q[2 * G], d = q[3 * G];
+      f(a); f(b); f(c); f(d);
+    }
+    for (; left > 0; left -= G, q += G) f(*q);
   }
 };
 
@@ -212,69 +211,108 @@ template <int G> __device__ __forceinline__ void group_sync() {
   else __syncthreads();
 }
 
-// Sums with the maximum known: s = sum e, t = sum e d, e = 2^d, d = (x - m) log2(e) / tau.  The difference is taken before the product: x c - m c in
-// one fused operation would be half an instruction per logit less, but rounds m c, which a row far from 0 (or masked with -1e9) makes larger than d.
+// Sums with the maximum known: s = sum e, t = sum e d, e = 2^d, d = (x - m) log2(e) / tau = (x - m) c.
+//   Near: d is taken as x c - mc in one operation, mc = m c rounded.  That rounding (the slip, known exactly from another fused operation) moves all
+//   exponents of the row alike, so sums can be put right at the end, and it is small where |m c| is; that saves half an instruction per
+//   logit.  Rows farther from 0 (or masked with -1e9, or with the type's lowest value) take the difference first.
+constexpr float kNear = 4096.f;        // |m c| below which the slip is below 2^-12
 struct Sums { float s, t; };
-template <typename T, bool ENT> struct Summing {
-  uint64_t c2, m2, s[2], t[2];
-  __device__ __forceinline__ Summing(float c, float m) : c2(pack2(c, c)), m2(pack2(-m, -m)) { s[0] = s[1] = t[0] = t[1] = 0; }
-  __device__ __forceinline__ void add(const uint4& u) {
-    constexpr int P = Elem<T>::E / 2;
-    uint64_t f[P];
-    Elem<T>::unpack(u, f);
+template <bool NEAR> struct Expo {
+  uint64_t a, b;
+  __device__ __forceinline__ Expo(float m, float c) : a(pack2(c, c)), b(NEAR ? pack2(-(m * c), -(m * c)) : pack2(-m, -m)) {}
+  __device__ __forceinline__ uint64_t operator()(uint64_t x) const { return NEAR ? fma2(x, a, b) : mul2(add2(x, b), a); }
+  static __device__ __forceinline__ float slip(float m, float c) { return NEAR ? fmaf(m, c, -(m * c)) : 0.f; }   // d comes out too large by this
+};
+__device__ __forceinline__ uint64_t exp2_pair(uint64_t d) {
+  float a, b;
+  unpack2(d, a, b);
+  return pack2(exp2_fast(a), exp2_fast(b));
+}
+template <typename T, int G, bool ENT, bool NEAR> __device__ __forceinline__ Sums thread_sums(const Slice<T, G>& sl, float m, float c) {
+  constexpr int P = Elem<T>::E / 2;
+  const Expo<NEAR> ex(m, c);
+  uint64_t s[2] = {0, 0}, t[2] = {0, 0};
+  sl.each([&](const uint4& u) {
+    uint64_t x[P];
+    Elem<T>::unpack(u, x);
 #pragma unroll
     for (int i = 0; i < P; ++i) {
-      const uint64_t d = mul2(add2(f[i], m2), c2);
-      float a, b;
-      unpack2(d, a, b);
-      const uint64_t e = pack2(exp2_fast(a), exp2_fast(b));
+      const uint64_t d = ex(x[i]), e = exp2_pair(d);
       s[i & 1] = add2(s[i & 1], e);
-      if (ENT) t[i & 1] = fma2(e, pack2(fmaxf(a, -1e30f), fmaxf(b, -1e30f)), t[i & 1]);   // a logit of -inf adds 0, not 0 * -inf
+      if (ENT) t[i & 1] = fma2(e, d, t[i & 1]);
+    }
+  });
+  Sums r{0.f, 0.f};
+  float a, b;
+  unpack2(add2(s[0], s[1]), a, b);
+  r.s = a + b;
+  if (ENT) {
+    unpack2(add2(t[0], t[1]), a, b);
+    r.t = a + b;
+    if (r.t != r.t && r.s == r.s) {     // 0 * -inf: the thread has met logits of -inf, which add nothing
+      t[0] = 0;
+      sl.each([&](const uint4& u) {
+        uint64_t x[P];
+        Elem<T>::unpack(u, x);
+#pragma unroll
+        for (int i = 0; i < P; ++i) {
+          const uint64_t d = ex(x[i]);
+          unpack2(d, a, b);
+          t[0] = fma2(exp2_pair(d), pack2(fmaxf(a, -1e30f), fmaxf(b, -1e30f)), t[0]);
+        }
+      });
+      unpack2(t[0], a, b);
+      r.t = a + b;
     }
   }
-  __device__ __forceinline__ Sums total() const {
-    float a, b;
-    unpack2(add2(s[0], s[1]), a, b);
-    Sums r{a + b, 0.f};
-    if (ENT) { unpack2(add2(t[0], t[1]), a, b); r.t = a + b; }
-    return r;
-  }
-};
+  return r;
+}
+__device__ __forceinline__ bool is_near(float m, float c) { return fabsf(m * c) < kNear; }
 
 // What the parts of a row know of it, and what the whole row comes to.
 struct Part { float m, s, t; };
 struct Stat { float m, L, H, s; };
 __device__ __forceinline__ float safe_max(float m) { return m == -INFINITY ? 0.f : m; }
-template <bool ENT> __device__ __forceinline__ Stat stat_finish(const Part* parts, int n, float c) {
-  Stat r;
-  float s = parts[0].s, t = parts[0].t;
-  r.m = parts[0].m;
-  if (n > 1) {                          // a part's exponents were taken against its own maximum
-    for (int i = 1; i < n; ++i) r.m = fmaxf(r.m, parts[i].m);
-    const float m0 = safe_max(r.m);
-    s = t = 0.f;
-    for (int i = 0; i < n; ++i) {
-      const float up = (safe_max(parts[i].m) - m0) * c, f = exp2_fast(up);
-      if (parts[i].s == 0.f) continue;  // nothing but -inf (its up means nothing)
-      s = fmaf(parts[i].s, f, s);
-      if (ENT && f != 0.f) t = fmaf(fmaf(parts[i].s, up, parts[i].t), f, t);
-    }
-  }
-  r.s = s;
-  r.L = logf(s);
-  r.H = ENT ? (s == 0.f ? 0.f : r.L - kLn2 * (t / s)) : 0.f;
+template <bool ENT> __device__ __forceinline__ Stat stat_of(float m, float s, float t) {
+  Stat r{m, logf(s), 0.f, s};
+  if (ENT && s != 0.f) r.H = r.L - kLn2 * (t / s);
   return r;
+}
+// The whole row from its parts (at most 8), by a whole warp: a part's exponents were taken against its own maximum.
+template <bool ENT> __device__ __forceinline__ Stat stat_of_parts(const Part* parts, int n, float c, int lane) {
+  Part p{-INFINITY, 0.f, 0.f};
+  if (lane < n) p = parts[lane];
+  const float m = warp_max(p.m);
+  const float up = (safe_max(p.m) - safe_max(m)) * c, f = p.s == 0.f ? 0.f : exp2_fast(up);   // s = 0: nothing but -inf, its up means nothing
+  float s = p.s * f, t = ENT && f != 0.f ? fmaf(p.s, up, p.t) * f : 0.f;
+#pragma unroll
+  for (int o = kMaxCluster / 2; o > 0; o >>= 1) {
+    s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
+    if (ENT) t += __shfl_xor_sync(0xFFFFFFFFu, t, o);
+  }
+  s = __shfl_sync(0xFFFFFFFFu, s, 0);
+  if (ENT) t = __shfl_sync(0xFFFFFFFFu, t, 0);
+  return stat_of<ENT>(m, s, t);
+}
+
+// The row's copy has arrived.  A wait that runs out is reported; it is waited for once more, so that no copy lands after the kernel.
+__device__ __forceinline__ void row_wait(uint64_t* bar, int32_t* status) {
+  if (mbar_wait(bar, 0)) return;
+  put_status(status, DEV_TIMEOUT_TMA);
+  mbar_wait(bar, 0);
 }
 
 // ---- scratch of a group beside its slice ---------------------------------------------------------------------------------
-constexpr int kThreadGroups = 128;                       // groups of threads whose maxima bound the alternatives from below (G > 32)
+constexpr int kFewAlt = 24;        // up to here the alternatives are bounded by the maxima of 32 groups of threads, beyond by those of 128
+constexpr int kThreadGroups = 128;
 template <int G, bool ALT> struct alignas(16) Scratch {
-  static constexpr int kCand = !ALT ? 0 : G == 32 ? 512 : 1024;
+  static constexpr int kCand = !ALT ? 0 : G == 32 ? 256 : 1024;
   float gm[ALT && G > 32 ? kThreadGroups : 4];
   float2 red[G / 32];
   float red_m[G / 32];
   float m, thr;
   int count;
+  unsigned long long bar;
   Part part[kMaxCluster];
   unsigned long long best[ALT ? G / 32 : 1];
   unsigned long long list[ALT ? kMaxAlt : 1];
@@ -286,8 +324,7 @@ template <int G, bool ALT> struct alignas(16) Scratch {
 template <typename T, int G, bool ALT> __device__ __forceinline__ float part_max(const Slice<T, G>& sl, Scratch<G, ALT>& sc, float mine) {
   float m = warp_max(mine);
   if constexpr (G > 32) {
-    const int warp = sl.t >> 5;
-    if ((sl.t & 31) == 0) sc.red_m[warp] = m;
+    if ((sl.t & 31) == 0) sc.red_m[sl.t >> 5] = m;
     __syncthreads();
     m = sc.red_m[0];
 #pragma unroll
@@ -295,23 +332,37 @@ template <typename T, int G, bool ALT> __device__ __forceinline__ float part_max
   }
   return m;
 }
-// The same, and a value that at least n_alt of the part's elements reach: the n_alt-th largest among the maxima of 32 (a warp) or 128 groups of
-// threads.  About n_alt (1 + n_alt / groups / 2) elements reach it where large values are spread over the row.  kLowest where fewer groups have a value.
+// The warp's values in descending order of the lanes (a bitonic network).
+__device__ __forceinline__ float sort_descending(float v, int lane) {
+#pragma unroll
+  for (int k = 2; k <= 32; k *= 2)
+#pragma unroll
+    for (int j = k / 2; j > 0; j /= 2) {
+      const float o = __shfl_xor_sync(0xFFFFFFFFu, v, j);
+      v = ((lane & j) == 0) == ((lane & k) == 0) ? fmaxf(v, o) : fminf(v, o);
+    }
+  return v;
+}
+// The maximum, and a value that at least n_alt of the part's elements reach: the n_alt-th largest among the maxima of groups of threads.  Where large
+// values are spread over the row, 1.2 n_alt elements reach that of 128 groups at n_alt 64, 1.8 n_alt that of 32 at 24 (of 24 at 24: 3.8 n_alt).  kLowest where fewer
+// groups have a value.
 template <typename T, int G> __device__ __forceinline__ float part_max_and_threshold(const Slice<T, G>& sl, Scratch<G, true>& sc, float mine, int n_alt, float& thr) {
   float m;
-  if constexpr (G == 32) {
-    int rank = 0;
-    m = mine;
+  const int lane = sl.t & 31;
+  if (G == 32 || n_alt <= kFewAlt) {
+    float g = mine;
+    if constexpr (G > 32) {
+      constexpr int SG = G / 32;
 #pragma unroll
-    for (int o = 1; o < 32; ++o) {
-      const int src = (sl.t + o) & 31;
-      const float v = __shfl_sync(0xFFFFFFFFu, mine, src);
-      rank += v > mine || (v == mine && src < sl.t);
-      m = fmaxf(m, v);
+      for (int o = SG / 2; o > 0; o >>= 1) g = fmaxf(g, __shfl_xor_sync(0xFFFFFFFFu, g, o));
+      if (sl.t % SG == 0) sc.gm[sl.t / SG] = g;
+      __syncthreads();
+      g = sc.gm[lane];
     }
-    const uint32_t who = __ballot_sync(0xFFFFFFFFu, rank == n_alt - 1);
-    thr = n_alt <= 32 ? __shfl_sync(0xFFFFFFFFu, mine, __ffs(who) - 1) : -INFINITY;
-  } else {
+    g = sort_descending(g, lane);
+    m = __shfl_sync(0xFFFFFFFFu, g, 0);
+    thr = __shfl_sync(0xFFFFFFFFu, g, n_alt - 1);
+  } else if constexpr (G > 32) {
     constexpr int SG = G / kThreadGroups;
     float g = mine;
 #pragma unroll
@@ -338,24 +389,56 @@ template <typename T, int G> __device__ __forceinline__ float part_max_and_thres
   return m;
 }
 
-template <int G, bool ALT> __device__ __forceinline__ Sums part_sums(int t, Scratch<G, ALT>& sc, Sums mine, bool ent) {
-  mine.s = warp_sum(mine.s);
-  if (ent) mine.t = warp_sum(mine.t);
+// The sums of the group's part against m, in every thread.
+template <bool ENT, typename T, int G, bool ALT> __device__ __forceinline__ Sums part_sums(const Slice<T, G>& sl, Scratch<G, ALT>& sc, float m, float c) {
+  const bool near = is_near(m, c);
+  Sums r = near ? thread_sums<T, G, ENT, true>(sl, m, c) : thread_sums<T, G, ENT, false>(sl, m, c);
+  r.s = warp_sum(r.s);
+  if (ENT) r.t = warp_sum(r.t);
   if constexpr (G > 32) {
-    if ((t & 31) == 0) sc.red[t >> 5] = make_float2(mine.s, mine.t);
+    if ((sl.t & 31) == 0) sc.red[sl.t >> 5] = make_float2(r.s, r.t);
     __syncthreads();
-    mine = {0.f, 0.f};
+    r = {0.f, 0.f};
 #pragma unroll
-    for (int w = 0; w < G / 32; ++w) { mine.s += sc.red[w].x; mine.t += sc.red[w].y; }
+    for (int w = 0; w < G / 32; ++w) { r.s += sc.red[w].x; r.t += sc.red[w].y; }
   } else {
     __syncwarp();
   }
-  return mine;
+  if (near) {
+    const float slip = Expo<true>::slip(m, c), f = fmaf(-kLn2, slip, 1.f);   // 2^-slip
+    if (ENT) r.t = fmaf(-slip, r.s, r.t) * f;
+    r.s *= f;
+  }
+  return r;
 }
 
 template <typename T> __device__ __forceinline__ float slice_elem(const uint4* s, int v, int e) {
   if constexpr (sizeof(T) == 4) return reinterpret_cast<const float*>(s + v)[e];
   else return __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(s + v)[e]);
+}
+
+// The keys of the part's elements that reach the threshold, in any order.  Few threads hold one; a warp goes over the vectors of each such thread together.
+template <typename T, int G> __device__ __forceinline__ void part_candidates(const Slice<T, G>& sl, Scratch<G, true>& sc, float mine, float thr) {
+  const int lane = sl.t & 31;
+  for (uint32_t who = __ballot_sync(0xFFFFFFFFu, mine >= thr); who; who &= who - 1) {
+    for (int v = (sl.t & ~31) + __ffs(who) - 1 + lane * G; v < sl.n; v += 32 * G) {
+      const uint4 u = sl.s[v];
+      uint64_t x[Elem<T>::E / 2];
+      Elem<T>::unpack(u, x);
+      const int i0 = sl.first_index(v);
+#pragma unroll
+      for (int e = 0; e < Elem<T>::E; ++e) {
+        float a, b;
+        unpack2(x[e >> 1], a, b);
+        const float f = e & 1 ? b : a;
+        if (f >= thr) {
+          const int slot = atomicAdd(&sc.count, 1);
+          if (slot < Scratch<G, true>::kCand) sc.cand[slot] = alt_key(f, i0 + e);
+        }
+      }
+    }
+  }
+  group_sync<G>();
 }
 
 // list[0 ... n_alt): the keys of the part's largest elements in descending order, 0 where there are fewer.  From the elements that reached the
@@ -404,14 +487,14 @@ template <typename T, int G> __device__ __forceinline__ void part_list(const Sli
 
 // ---- log probabilities of given tokens, statistics, entropy, alternatives ------------------------------------------------
 struct RowsArgs {
-  const void* x; long long ld; int rows, V, per_max;   // per_max: vectors of the largest slice
+  const void* x; long long ld; int rows, V, per_max, lg;   // per_max: vectors of the largest slice; lg: of the CTAs that share a row, the logarithm
   float inv_tau;
   const int32_t* ids; int n_alt;
   float* logprob; float2* stats; float* entropy; int32_t* alt_ids; float* alt_logprob;
   int32_t* status;
 };
 
-constexpr int kWarpRows = 4;       // rows of a CTA where a warp takes one
+constexpr int kWarpRows = 2;       // rows of a CTA where a warp takes one
 template <int G> constexpr int cta_threads() { return G == 32 ? 32 * kWarpRows : G; }
 template <typename S> __host__ __device__ constexpr size_t group_bytes(int per_max) { return (size_t)per_max * 16 + sizeof(S); }
 
@@ -420,62 +503,48 @@ __global__ void __launch_bounds__(cta_threads<G>()) token_logprobs_kernel(const 
   using S = Scratch<G, ALT>;
   extern __shared__ uint4 smem[];
   pdl_trigger();
-  const int parts = G == 32 ? 1 : (int)cluster_nctas(), rank = G == 32 ? 0 : (int)cluster_ctarank();
+  const int parts = G == 32 ? 1 : 1 << p.lg, rank = G == 32 ? 0 : (int)cluster_ctarank();
   const int sub = G == 32 ? threadIdx.x >> 5 : 0, t = G == 32 ? threadIdx.x & 31 : threadIdx.x;
-  const int row = G == 32 ? blockIdx.x * kWarpRows + sub : blockIdx.x / parts;
+  const int row = G == 32 ? blockIdx.x * kWarpRows + sub : blockIdx.x >> p.lg;
   pdl_wait();
   if (G == 32 && row >= p.rows) return;
   if (G > 32 && parts > 1) cluster_arrive_relaxed();
   uint4* mine = reinterpret_cast<uint4*>(reinterpret_cast<char*>(smem) + sub * group_bytes<S>(p.per_max));
   S& sc = *reinterpret_cast<S*>(mine + p.per_max);
   const T* xrow = static_cast<const T*>(p.x) + row * p.ld;
-  Slice<T, G> sl(xrow, p.V, rank, parts, t, mine);
-  sl.fetch();
+  Slice<T, G> sl(xrow, p.V, rank, G == 32 ? 0 : p.lg, t, mine);
+  uint64_t* bar = reinterpret_cast<uint64_t*>(&sc.bar);
+  if (t == 0) { mbar_init(bar, 1); mbar_fence_init(); }
+  if (ALT) {
+    if (t < kMaxAlt) sc.list[t] = 0;
+    if (G == 32) sc.list[t + 32] = 0;
+    if (t == 0) sc.count = 0;
+  }
+  group_sync<G>();
+  sl.fetch(bar);
   float xid = 0.f;
   int id = -1;
   if (t == 0 && rank == 0 && p.ids) {
     id = dep_load(p.ids + row);
     if (id >= 0 && id < p.V) xid = Elem<T>::load(xrow + id);
   }
-  if (ALT) {
-    if (t < kMaxAlt) sc.list[t] = 0;
-    if (G == 32) sc.list[t + 32] = 0;
-    if (t == 0) sc.count = 0;
-    if (G == 32) __syncwarp();
-  }
-  cp_async_wait_all();
+  row_wait(bar, p.status);
   typename Elem<T>::Max mx;
-  for (int v = t; v < sl.n; v += G) mx.add(mine[v]);
+  sl.each([&](const uint4& u) { mx.add(u); });
+  const float own = mx.value(), c = p.inv_tau * kLog2e;
   float m, thr = 0.f;
-  if constexpr (ALT) m = part_max_and_threshold<T, G>(sl, sc, mx.value(), p.n_alt, thr);
-  else m = part_max<T, G, ALT>(sl, sc, mx.value());
-  const float c = p.inv_tau * kLog2e;
-  Summing<T, ENT> sum(c, safe_max(m));
-  typename Elem<T>::AtLeast reach(thr);
-#pragma unroll 2
-  for (int v = t; v < sl.n; v += G) {
-    const uint4 u = mine[v];
-    sum.add(u);
-    if (ALT && reach.any(u)) {
-      const int i0 = sl.first_index(v);
-      for (int e = 0; e < Elem<T>::E; ++e) {
-        const float x = slice_elem<T>(mine, v, e);
-        if (x >= thr) {
-          const int slot = atomicAdd(&sc.count, 1);
-          if (slot < S::kCand) sc.cand[slot] = alt_key(x, i0 + e);
-        }
-      }
-    }
+  if constexpr (ALT) m = part_max_and_threshold<T, G>(sl, sc, own, p.n_alt, thr);
+  else m = part_max<T, G, ALT>(sl, sc, own);
+  const Sums tot = part_sums<ENT>(sl, sc, safe_max(m), c);
+  if constexpr (ALT) {
+    part_candidates<T, G>(sl, sc, own, thr);
+    part_list<T, G>(sl, sc, p.n_alt);
   }
-  const Sums tot = part_sums<G, ALT>(t, sc, sum.total(), ENT);
-  if constexpr (ALT) part_list<T, G>(sl, sc, p.n_alt);
   const Part part{m, tot.s, tot.t};
   Stat st;
   unsigned long long* alts = sc.list;
-  if constexpr (G == 32) {
-    st = stat_finish<ENT>(&part, 1, c);
-  } else if (parts == 1) {
-    st = stat_finish<ENT>(&part, 1, c);
+  if (G == 32 || parts == 1) {
+    st = stat_of<ENT>(m, tot.s, tot.t);
   } else {
     __syncwarp();
     cluster_wait();                      // every CTA of the cluster has started
@@ -487,7 +556,7 @@ __global__ void __launch_bounds__(cta_threads<G>()) token_logprobs_kernel(const 
     __syncwarp();
     cluster_sync_all();
     if (rank != 0) return;
-    st = stat_finish<ENT>(sc.part, parts, c);
+    st = stat_of_parts<ENT>(sc.part, parts, c, t & 31);
     if constexpr (ALT) {                 // a key's place: its own, and how many of each other list are larger
       alts = sc.cand;
       if (t < p.n_alt) alts[t] = 0;
@@ -537,7 +606,7 @@ __global__ void __launch_bounds__(cta_threads<G>()) token_logprobs_kernel(const 
 
 // ---- distillation: loss, and with GRAD its gradient while the row is still in shared memory --------------------------------
 struct DistillArgs {
-  const void* x; long long ld; int rows, V, per_max;
+  const void* x; long long ld; int rows, V, per_max, lg;
   float inv_tau;
   const int32_t* t_ids; const float* t_logits; int K;
   const float* g;                  // [rows] or null: 1
@@ -560,6 +629,7 @@ struct Teacher {
       const int k = lane + 32 * i;
       id[i] = -1;
       x[i] = -INFINITY;
+      if (32 * i >= K) continue;
       if (k < K) {
         const int v = dep_load(ids + k);
         if (v >= 0 && v < V) {
@@ -575,30 +645,42 @@ struct Teacher {
     m = safe_max(warp_max(m));
     float s = 0.f;
 #pragma unroll
-    for (int i = 0; i < P; ++i) { lq[i] = (x[i] - m) * inv_tau; q[i] = expf(lq[i]); s += q[i]; }
+    for (int i = 0; i < P; ++i) {
+      lq[i] = q[i] = 0.f;
+      if (32 * i >= K) continue;
+      lq[i] = (x[i] - m) * inv_tau;
+      q[i] = expf(lq[i]);
+      s += q[i];
+    }
     s = warp_sum(s);
     some = __any_sync(0xFFFFFFFFu, any);
     bad = __any_sync(0xFFFFFFFFu, wrong);
     const float ls = logf(s);
 #pragma unroll
-    for (int i = 0; i < P; ++i) { q[i] = some ? q[i] / s : 0.f; lq[i] -= ls; }
+    for (int i = 0; i < P; ++i) {
+      if (32 * i >= K) continue;
+      q[i] = some ? q[i] / s : 0.f;
+      lq[i] -= ls;
+    }
   }
 };
-struct TeacherRow {                // of one row, for the gradient's corrections
+struct alignas(16) TeacherRow {    // of one row, for the gradient's corrections
   int id[kMaxTeacher];
   float q[kMaxTeacher], x[kMaxTeacher];
   int some;
 };
-// What entry k takes off its token's probability: all entries of that token together, at the first of them; -1 elsewhere.
+// What entry k, which has a token, takes off its probability: all entries of that token together, at the first of them; -1 elsewhere.
 __device__ __forceinline__ float teacher_share(const TeacherRow& tr, int k, int K) {
   const int id = tr.id[k];
-  if (id < 0) return -1.f;
   float sum = 0.f;
   bool first = true;
-  for (int j = 0; j < K; ++j) {
-    const bool same = tr.id[j] == id;
-    first &= !(same && j < k);
-    sum += same ? tr.q[j] : 0.f;
+  for (int j = 0; j < K; j += 4) {         // (behind K: id -1)
+    const int4 o = *reinterpret_cast<const int4*>(tr.id + j);
+    const float4 q = *reinterpret_cast<const float4*>(tr.q + j);
+    if (o.x == id) { sum += q.x; first &= j >= k; }
+    if (o.y == id) { sum += q.y; first &= j + 1 >= k; }
+    if (o.z == id) { sum += q.z; first &= j + 2 >= k; }
+    if (o.w == id) { sum += q.w; first &= j + 3 >= k; }
   }
   return first ? sum : -1.f;
 }
@@ -607,14 +689,41 @@ template <typename T> __device__ __forceinline__ bool same_alignment(const T* a,
   return ((reinterpret_cast<uintptr_t>(a) ^ reinterpret_cast<uintptr_t>(b)) & 15u) == 0;
 }
 
+// f of every pair of logits of the part, written where the row's gradient lies.
+template <typename T, int G, typename F> __device__ __forceinline__ void write_row(const Slice<T, G>& sl, T* drow, F f) {
+  constexpr int E = Elem<T>::E, P = E / 2;
+  const bool vec = same_alignment(sl.row, static_cast<const T*>(drow));
+  T* dvec = drow - sl.off + (size_t)sl.v0 * E;
+#pragma unroll 4
+  for (int v = sl.t; v < sl.n; v += G) {
+    uint64_t d[P];
+    Elem<T>::unpack(sl.s[v], d);
+#pragma unroll
+    for (int i = 0; i < P; ++i) d[i] = f(d[i]);
+    if (vec && sl.whole(v)) {
+      *reinterpret_cast<uint4*>(dvec + (size_t)v * E) = Elem<T>::pack(d);
+    } else {
+      const int i0 = sl.first_index(v);
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        float a, b;
+        unpack2(d[e >> 1], a, b);
+        if (i0 + e >= 0 && i0 + e < sl.V) Elem<T>::store(drow + i0 + e, e & 1 ? b : a);
+      }
+    }
+  }
+}
+
+template <int G> struct alignas(16) DistillScratch { Scratch<G, false> sc; TeacherRow tr; };
+
 template <typename T, int G, bool GRAD>
 __global__ void __launch_bounds__(cta_threads<G>()) distill_kernel(const DistillArgs p) {
-  struct alignas(16) S { Scratch<G, false> sc; TeacherRow tr; };
+  using S = DistillScratch<G>;
   extern __shared__ uint4 smem[];
   pdl_trigger();
-  const int parts = G == 32 ? 1 : (int)cluster_nctas(), rank = G == 32 ? 0 : (int)cluster_ctarank();
+  const int parts = G == 32 ? 1 : 1 << p.lg, rank = G == 32 ? 0 : (int)cluster_ctarank();
   const int sub = G == 32 ? threadIdx.x >> 5 : 0, t = G == 32 ? threadIdx.x & 31 : threadIdx.x;
-  const int row = G == 32 ? blockIdx.x * kWarpRows + sub : blockIdx.x / parts;
+  const int row = G == 32 ? blockIdx.x * kWarpRows + sub : blockIdx.x >> p.lg;
   pdl_wait();
   if (G == 32 && row >= p.rows) return;
   if (G > 32 && parts > 1) cluster_arrive_relaxed();
@@ -623,32 +732,32 @@ __global__ void __launch_bounds__(cta_threads<G>()) distill_kernel(const Distill
   Scratch<G, false>& sc = own.sc;
   TeacherRow& tr = own.tr;
   const T* xrow = static_cast<const T*>(p.x) + row * p.ld;
-  Slice<T, G> sl(xrow, p.V, rank, parts, t, mine);
-  sl.fetch();
+  Slice<T, G> sl(xrow, p.V, rank, G == 32 ? 0 : p.lg, t, mine);
+  uint64_t* bar = reinterpret_cast<uint64_t*>(&sc.bar);
+  if (t == 0) { mbar_init(bar, 1); mbar_fence_init(); }
+  group_sync<G>();
+  sl.fetch(bar);
   Teacher te;
   float xk[Teacher::P];
   if (t < 32 && (GRAD || rank == 0)) {
     te.load(p.t_ids + (size_t)row * p.K, p.t_logits + (size_t)row * p.K, p.K, p.V, p.inv_tau, t);
 #pragma unroll
     for (int i = 0; i < Teacher::P; ++i) {
-      xk[i] = te.id[i] >= 0 ? Elem<T>::load(xrow + te.id[i]) : 0.f;
+      xk[i] = 0.f;
+      if (GRAD || 32 * i < p.K) xk[i] = te.id[i] >= 0 ? Elem<T>::load(xrow + te.id[i]) : 0.f;
       if (GRAD) { tr.id[t + 32 * i] = te.id[i]; tr.q[t + 32 * i] = te.q[i]; tr.x[t + 32 * i] = xk[i]; }
     }
     if (GRAD && t == 0) tr.some = te.some;
   }
-  cp_async_wait_all();
+  row_wait(bar, p.status);
   typename Elem<T>::Max mx;
-  for (int v = t; v < sl.n; v += G) mx.add(mine[v]);
-  const float m = part_max<T, G, false>(sl, sc, mx.value());
-  const float c = p.inv_tau * kLog2e;
-  Summing<T, false> sum(c, safe_max(m));
-#pragma unroll 2
-  for (int v = t; v < sl.n; v += G) sum.add(mine[v]);
-  const Sums tot = part_sums<G, false>(t, sc, sum.total(), false);
+  sl.each([&](const uint4& u) { mx.add(u); });
+  const float m = part_max<T, G, false>(sl, sc, mx.value()), c = p.inv_tau * kLog2e;
+  const Sums tot = part_sums<false>(sl, sc, safe_max(m), c);
   const Part part{m, tot.s, 0.f};
   Stat st;
   if (G == 32 || parts == 1) {
-    st = stat_finish<false>(&part, 1, c);
+    st = stat_of<false>(m, tot.s, 0.f);
   } else {
     __syncwarp();
     cluster_wait();
@@ -659,7 +768,7 @@ __global__ void __launch_bounds__(cta_threads<G>()) distill_kernel(const Distill
     __syncwarp();
     cluster_sync_all();                  // in place: and every CTA has read the logits of the teacher's tokens
     if (!GRAD && rank != 0) return;
-    st = stat_finish<false>(sc.part, parts, c);
+    st = stat_of_parts<false>(sc.part, parts, c, t & 31);
   }
   if (rank == 0 && t < 32) {
     float loss = 0.f;
@@ -676,36 +785,15 @@ __global__ void __launch_bounds__(cta_threads<G>()) distill_kernel(const Distill
     }
   }
   if constexpr (GRAD) {
-    constexpr int E = Elem<T>::E, P = E / 2;
+    constexpr int E = Elem<T>::E;
     T* drow = static_cast<T*>(p.dx) + row * p.ld_dx;
     const float w = (p.g ? dep_load(p.g + row) : 1.f) * p.inv_tau;
     const bool none = !tr.some || w == 0.f || st.L == -INFINITY;   // (tr: written before the barriers of the sums)
-    const float f = none ? 0.f : w / st.s;
-    const uint64_t c2 = pack2(c, c), m2 = pack2(-st.m, -st.m), f2 = pack2(f, f);
-    const bool vec = same_alignment(xrow, drow);
-    T* dvec = drow - sl.off + (size_t)sl.v0 * E;
-#pragma unroll 2
-    for (int v = t; v < sl.n; v += G) {
-      uint64_t d[P];
-      Elem<T>::unpack(mine[v], d);
-#pragma unroll
-      for (int i = 0; i < P; ++i) {
-        float a, b;
-        unpack2(mul2(add2(d[i], m2), c2), a, b);
-        d[i] = none ? 0 : mul2(pack2(exp2_fast(a), exp2_fast(b)), f2);
-      }
-      if (vec && sl.whole(v)) {
-        *reinterpret_cast<uint4*>(dvec + (size_t)v * E) = Elem<T>::pack(d);
-      } else {
-        const int i0 = sl.first_index(v);
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-          float a, b;
-          unpack2(d[e >> 1], a, b);
-          if (i0 + e >= 0 && i0 + e < p.V) Elem<T>::store(drow + i0 + e, e & 1 ? b : a);
-        }
-      }
-    }
+    const bool near = is_near(st.m, c);
+    const float f = none ? 0.f : near ? w / st.s * fmaf(-kLn2, Expo<true>::slip(st.m, c), 1.f) : w / st.s;
+    if (none) write_row<T, G>(sl, drow, [&](uint64_t) { return uint64_t(0); });
+    else if (near) write_row<T, G>(sl, drow, [&, ex = Expo<true>(st.m, c), f2 = pack2(f, f)](uint64_t x) { return mul2(exp2_pair(ex(x)), f2); });
+    else write_row<T, G>(sl, drow, [&, ex = Expo<false>(st.m, c), f2 = pack2(f, f)](uint64_t x) { return mul2(exp2_pair(ex(x)), f2); });
     group_sync<G>();
     if (!none)
       for (int k = t; k < p.K; k += G) {
@@ -714,7 +802,7 @@ __global__ void __launch_bounds__(cta_threads<G>()) distill_kernel(const Distill
         if (at < 0 || at >= sl.n) continue;
         const float share = teacher_share(tr, k, p.K);
         if (share < 0.f) continue;
-        Elem<T>::store(drow + id, fmaf(exp2_fast((tr.x[k] - st.m) * c), f, -w * share));
+        Elem<T>::store(drow + id, w * (exp2_fast((tr.x[k] - st.m) * c) / st.s - share));
       }
   }
 }
@@ -757,10 +845,8 @@ template <typename T, int U> struct Segment {
       } else if (v0 + 32 * u < nv) {
         uint64_t f[E / 2];
 #pragma unroll
-        for (int e = 0; e < E; e += 2) {
-          const bool a = i0 + e >= 0 && i0 + e < V, b = i0 + e + 1 >= 0 && i0 + e + 1 < V;
-          f[e / 2] = pack2(a ? Elem<T>::load(row + i0 + e) : 0.f, b ? Elem<T>::load(row + i0 + e + 1) : 0.f);
-        }
+        for (int e = 0; e < E; e += 2)
+          f[e / 2] = pack2(Elem<T>::load(row + min(max(i0 + e, 0), V - 1)), Elem<T>::load(row + min(max(i0 + e + 1, 0), V - 1)));
         x[u] = Elem<T>::pack(f);
       }
     }
@@ -869,7 +955,7 @@ __global__ void __launch_bounds__(32 * kGradWarps) distill_grad_kernel(const Gra
     sg.zero();
     return;
   }
-  const int lo = (seg * 32 * U) * E - sg.off, hi = min(p.V, lo + 32 * U * E);   // the logits of this warp
+  const int from = seg * 32 * U * E - sg.off, lo = max(0, from), hi = min(p.V, from + 32 * U * E);   // the logits of this warp
 #pragma unroll
   for (int i = 0; i < Teacher::P; ++i) {
     const int id = te.id[i];
@@ -918,16 +1004,21 @@ cudaError_t launch_clusters(void (*kernel)(KArgs...), unsigned grid, int threads
   return cudaLaunchKernelEx(&cfg, kernel, static_cast<KArgs>(args)...);
 }
 
-// Who takes a row: a warp, or a cluster of CTAs of 256 threads.
-struct Shape { int group, cluster, per_max; };
+// Who takes a row: a warp, or a cluster of CTAs of 128 or 256 threads.
+struct Shape { int group, lg, per_max; };
 constexpr int kMaxRowBytes = 1536 << 10;
-Shape row_shape(int rows, int V, int es, bool warp_may) {
-  const int nv = logits_vectors(V, 16 / es);
-  if (warp_may && nv <= 1024 && rows >= 148 * 8) return {32, 1, nv};
-  int s = 1;
-  while (s < kMaxCluster && (size_t)(nv + s - 1) / s * 16 > (48 << 10)) s *= 2;
-  while (s < kMaxCluster && (long long)rows * s < 148 && nv / (2 * s) >= 512) s *= 2;
-  return {256, s, (nv + s - 1) / s};
+static int envi(const char* n, int d) { const char* s = getenv(n); return s ? atoi(s) : d; }
+Shape row_shape(const void* x, long long ld, int rows, int V, int es, bool warp_may) {
+  const int E = 16 / es;
+  const bool aligned = (reinterpret_cast<uintptr_t>(x) & 15u) == 0 && (ld * es) % 16 == 0;   // every row starts on a boundary
+  const int nv = aligned ? (V + E - 1) / E : logits_vectors(V, E);
+  static const int WV = envi("FV_WV", 1024), G1 = envi("FV_G1", 128), N1 = envi("FV_N1", 2048), SL = envi("FV_SL", 48), WR = envi("FV_WR", 8), LM = envi("FV_LM", 512);
+  if (warp_may && nv <= WV && rows >= 148 * WR) return {32, 0, nv};
+  int lg = 0;
+  while ((1 << lg) < kMaxCluster && (size_t)((nv + (1 << lg) - 1) >> lg) * 16 > ((size_t)SL << 10)) ++lg;
+  while ((1 << lg) < kMaxCluster && ((long long)rows << lg) < 148 && (nv >> (lg + 1)) >= LM) ++lg;
+  const int per = (nv + (1 << lg) - 1) >> lg;
+  return {per <= N1 ? G1 : 256, lg, per};
 }
 
 constexpr int kMaxSmem = 227 << 10;
@@ -935,12 +1026,13 @@ template <typename K> cudaError_t allow_smem(K kernel) { return cudaFuncSetAttri
 template <typename T> cudaError_t allow_all() {
   cudaError_t e = cudaSuccess;
   auto add = [&](auto kernel) { if (e == cudaSuccess) e = allow_smem(kernel); };
-  add(token_logprobs_kernel<T, 32, false, false>); add(token_logprobs_kernel<T, 32, false, true>);
-  add(token_logprobs_kernel<T, 32, true, false>); add(token_logprobs_kernel<T, 32, true, true>);
-  add(token_logprobs_kernel<T, 256, false, false>); add(token_logprobs_kernel<T, 256, false, true>);
-  add(token_logprobs_kernel<T, 256, true, false>); add(token_logprobs_kernel<T, 256, true, true>);
-  add(distill_kernel<T, 32, false>); add(distill_kernel<T, 32, true>);
-  add(distill_kernel<T, 256, false>); add(distill_kernel<T, 256, true>);
+  auto group = [&](auto g) {
+    constexpr int G = decltype(g)::value;
+    add(token_logprobs_kernel<T, G, false, false>); add(token_logprobs_kernel<T, G, false, true>);
+    add(token_logprobs_kernel<T, G, true, false>); add(token_logprobs_kernel<T, G, true, true>);
+    add(distill_kernel<T, G, false>); add(distill_kernel<T, G, true>);
+  };
+  group(std::integral_constant<int, 32>()); group(std::integral_constant<int, 128>()); group(std::integral_constant<int, 256>());
   return e;
 }
 // Function attributes belong to a device: set on the first call on each.
@@ -955,32 +1047,32 @@ cudaError_t logits_init() {
   return e;
 }
 
-template <typename T, int G, bool ENT, bool ALT> cudaError_t go_token(RowsArgs& a, const Shape& s, cudaStream_t st) {
-  const size_t smem = group_bytes<Scratch<G, ALT>>(s.per_max) * (G == 32 ? kWarpRows : 1);
-  const unsigned grid = G == 32 ? (a.rows + kWarpRows - 1) / kWarpRows : (unsigned)a.rows * s.cluster;
-  return launch_clusters(token_logprobs_kernel<T, G, ENT, ALT>, grid, cta_threads<G>(), s.cluster, smem, st, a);
+template <typename F> cudaError_t with_group(int group, F f) {
+  if (group == 32) return f(std::integral_constant<int, 32>());
+  return group == 128 ? f(std::integral_constant<int, 128>()) : f(std::integral_constant<int, 256>());
+}
+template <int G, typename K, typename A> cudaError_t go_rows(K kernel, const A& a, size_t bytes, cudaStream_t st) {   // bytes: of a group's shared memory
+  const unsigned grid = G == 32 ? (a.rows + kWarpRows - 1) / kWarpRows : (unsigned)a.rows << a.lg;
+  return launch_clusters(kernel, grid, cta_threads<G>(), 1 << a.lg, bytes * (G == 32 ? kWarpRows : 1), st, a);
 }
 template <typename T> cudaError_t launch_token(RowsArgs& a, cudaStream_t st) {
-  const Shape s = row_shape(a.rows, a.V, sizeof(T), a.n_alt <= 24);
-  a.per_max = s.per_max;
-  const bool ent = a.entropy != nullptr, alt = a.n_alt > 0;
-  if (s.group == 32)
-    return ent ? (alt ? go_token<T, 32, true, true>(a, s, st) : go_token<T, 32, true, false>(a, s, st))
-               : (alt ? go_token<T, 32, false, true>(a, s, st) : go_token<T, 32, false, false>(a, s, st));
-  return ent ? (alt ? go_token<T, 256, true, true>(a, s, st) : go_token<T, 256, true, false>(a, s, st))
-             : (alt ? go_token<T, 256, false, true>(a, s, st) : go_token<T, 256, false, false>(a, s, st));
-}
-template <typename T, int G, bool GRAD> cudaError_t go_distill(DistillArgs& a, const Shape& s, cudaStream_t st) {
-  struct alignas(16) S { Scratch<G, false> sc; TeacherRow tr; };   // as in the kernel
-  const size_t smem = group_bytes<S>(s.per_max) * (G == 32 ? kWarpRows : 1);
-  const unsigned grid = G == 32 ? (a.rows + kWarpRows - 1) / kWarpRows : (unsigned)a.rows * s.cluster;
-  return launch_clusters(distill_kernel<T, G, GRAD>, grid, cta_threads<G>(), s.cluster, smem, st, a);
+  const Shape s = row_shape(a.x, a.ld, a.rows, a.V, sizeof(T), a.n_alt <= kFewAlt);
+  a.per_max = s.per_max; a.lg = s.lg;
+  return with_group(s.group, [&](auto g) {
+    constexpr int G = decltype(g)::value;
+    const size_t with = group_bytes<Scratch<G, true>>(s.per_max), without = group_bytes<Scratch<G, false>>(s.per_max);
+    if (a.n_alt > 0) return a.entropy ? go_rows<G>(token_logprobs_kernel<T, G, true, true>, a, with, st) : go_rows<G>(token_logprobs_kernel<T, G, false, true>, a, with, st);
+    return a.entropy ? go_rows<G>(token_logprobs_kernel<T, G, true, false>, a, without, st) : go_rows<G>(token_logprobs_kernel<T, G, false, false>, a, without, st);
+  });
 }
 template <typename T> cudaError_t launch_distill(DistillArgs& a, cudaStream_t st) {
-  const Shape s = row_shape(a.rows, a.V, sizeof(T), true);
-  a.per_max = s.per_max;
-  if (s.group == 32) return a.dx ? go_distill<T, 32, true>(a, s, st) : go_distill<T, 32, false>(a, s, st);
-  return a.dx ? go_distill<T, 256, true>(a, s, st) : go_distill<T, 256, false>(a, s, st);
+  const Shape s = row_shape(a.x, a.ld, a.rows, a.V, sizeof(T), true);
+  a.per_max = s.per_max; a.lg = s.lg;
+  return with_group(s.group, [&](auto g) {
+    constexpr int G = decltype(g)::value;
+    const size_t bytes = group_bytes<DistillScratch<G>>(s.per_max);
+    return a.dx ? go_rows<G>(distill_kernel<T, G, true>, a, bytes, st) : go_rows<G>(distill_kernel<T, G, false>, a, bytes, st);
+  });
 }
 template <typename T, int U, typename K> cudaError_t launch_grad(K kernel, GradArgs& a, cudaStream_t st) {
   a.segs = (logits_vectors(a.V, Elem<T>::E) + 32 * U - 1) / (32 * U);
@@ -1019,7 +1111,7 @@ fv_status fv_token_logprobs(const void* logits_dev, int32_t dtype, int64_t ld, i
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const double bytes = (double)rows * ((dtype ? 2.0 : 4.0) * V + 20.0 + 8.0 * n_alt);
   LaunchScope scope(KC_SELECT, 1, bytes, bytes, st);
-  RowsArgs a{logits_dev, ld, rows, V, 0, 1.f / tau, ids_dev, n_alt, logprob_out_dev, reinterpret_cast<float2*>(stats_out_dev), entropy_out_dev,
+  RowsArgs a{logits_dev, ld, rows, V, 0, 0, 1.f / tau, ids_dev, n_alt, logprob_out_dev, reinterpret_cast<float2*>(stats_out_dev), entropy_out_dev,
              alt_ids_out_dev, alt_logprob_out_dev, status_dev};
   return cu(dtype ? launch_token<__nv_bfloat16>(a, st) : launch_token<float>(a, st));
 }
@@ -1053,7 +1145,7 @@ fv_status fv_distill_topk(const void* logits_dev, int32_t dtype, int64_t ld, int
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const double bytes = (double)rows * ((dtype ? 2.0 : 4.0) * V * (dlogits_out_dev ? 2.0 : 1.0) + 8.0 * K + 16.0);
   LaunchScope scope(KC_SELECT, 1, bytes, bytes, st);
-  DistillArgs a{logits_dev, ld, rows, V, 0, 1.f / tau, teacher_ids_dev, teacher_logits_dev, K, g_loss_dev, loss_out_dev, reinterpret_cast<float2*>(stats_out_dev),
+  DistillArgs a{logits_dev, ld, rows, V, 0, 0, 1.f / tau, teacher_ids_dev, teacher_logits_dev, K, g_loss_dev, loss_out_dev, reinterpret_cast<float2*>(stats_out_dev),
                 dlogits_out_dev, ld_out, status_dev};
   return cu(dtype ? launch_distill<__nv_bfloat16>(a, st) : launch_distill<float>(a, st));
 }
