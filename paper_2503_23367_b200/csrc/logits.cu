@@ -15,7 +15,6 @@
 #include <cfloat>
 #include <climits>
 #include <cstdint>
-#include <cstdlib>
 #include <type_traits>
 
 #include "internal.h"
@@ -66,16 +65,17 @@ __device__ __forceinline__ float warp_sum(float v) {
   for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
   return v;
 }
-// Untiled copy global -> this CTA's shared memory, its bytes counted on `bar`.  Both addresses and the size are multiples of 16.
-__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint64_t* bar) {
-  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(smem_u32(bar)) : "memory");
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
+__device__ __forceinline__ void cp_async_wait_all() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 __device__ __forceinline__ uint32_t peer_smem(const void* p, uint32_t cta) {   // the same shared-memory address in another CTA of the cluster
   uint32_t r;
   asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(smem_u32(p)), "r"(cta));
   return r;
 }
 __device__ __forceinline__ void peer_store(uint32_t addr, float v) { asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(addr), "f"(v) : "memory"); }
+__device__ __forceinline__ void peer_store(uint32_t addr, int v) { asm volatile("st.shared::cluster.s32 [%0], %1;" ::"r"(addr), "r"(v) : "memory"); }
 __device__ __forceinline__ void peer_store(uint32_t addr, uint64_t v) { asm volatile("st.shared::cluster.b64 [%0], %1;" ::"r"(addr), "l"(v) : "memory"); }
 __device__ __forceinline__ void put_status(int32_t* status, int code) {
   if (status) atomicCAS(status, 0, code);
@@ -155,8 +155,8 @@ __device__ __forceinline__ int alt_index(uint64_t key) { return (int)(0xFFFFFFFF
 
 // ---- the part of a row that a group of G threads holds in shared memory ---------------------------------------------------
 // Vectors of 16 bytes counted from the row's start rounded down to 16 bytes, so a row may start anywhere; elements of the first and last
-// vector that are not the row's are -inf, which no pass notices.  The cluster's CTAs split the vectors evenly.  Thread t reads the
-// vectors t, t + G, ... of its part.
+// vector that are not the row's are -inf, which no pass notices.  The cluster's CTAs split the vectors evenly.  Thread t copies and reads the
+// vectors t, t + G, ... of its part, so it needs no barrier before its own passes.
 template <typename T, int G> struct Slice {
   static constexpr int E = Elem<T>::E;
   const T* row;      // first logit of the row
@@ -174,7 +174,17 @@ template <typename T, int G> struct Slice {
   }
   __device__ __forceinline__ int first_index(int v) const { return (v0 + v) * E - off; }   // index in the row of the vector's first element
   __device__ __forceinline__ bool whole(int v) const { return v != head && v != tail; }
-  __device__ __forceinline__ void build(int v) {
+  __device__ __forceinline__ void fetch() const {
+    const char* g = reinterpret_cast<const char*>(row - off) + (size_t)(v0 + t) * 16;
+    const uint32_t d = smem_u32(s + t);
+    const int left = n - t;
+#pragma unroll 4
+    for (int i = 0; i < left; i += G)
+      if (whole(t + i)) cp_async16(d + i * 16, g + (size_t)i * 16);
+    if (t == 0 && head == 0) build(0);
+    if (tail >= 0 && tail != head && tail % G == t) build(tail);
+  }
+  __device__ __forceinline__ void build(int v) const {   // a vector that is the row's in part
     T* d = reinterpret_cast<T*>(s + v);
     const int i0 = first_index(v);
     float x[E];
@@ -182,17 +192,6 @@ template <typename T, int G> struct Slice {
     for (int e = 0; e < E; ++e) x[e] = Elem<T>::load(row + min(max(i0 + e, 0), V - 1));   // all on their way before the first is stored
 #pragma unroll
     for (int e = 0; e < E; ++e) Elem<T>::store(d + e, i0 + e >= 0 && i0 + e < V ? x[e] : -INFINITY);
-  }
-  // One copy for all whole vectors, completed on `bar`; the partial ones are built by the threads that hold them.
-  __device__ __forceinline__ void fetch(uint64_t* bar) {
-    if (t == 0) {
-      const int lo = head == 0, hi = tail >= 0 ? max(n - 1, lo) : n;
-      const uint32_t bytes = (uint32_t)(hi - lo) * 16;
-      mbar_expect_tx(bar, bytes);
-      if (bytes) bulk_load(smem_u32(s + lo), reinterpret_cast<const char*>(row - off) + (size_t)(v0 + lo) * 16, bytes, bar);
-    }
-    if (t == 0 && head == 0) build(0);
-    if (tail >= 0 && tail != head && tail % G == t) build(tail);
   }
   // f(vector) for the thread's vectors, four loads at a time.
   template <typename F> __device__ __forceinline__ void each(F f) const {
@@ -204,441 +203,626 @@ template <typename T, int G> struct Slice {
     }
     for (; left > 0; left -= G, q += G) f(*q);
   }
+  __device__ __forceinline__ float element(int i) const {   // logit i of the row, which lies in this part
+    const int e = i + off - v0 * E;
+    if constexpr (sizeof(T) == 4) return reinterpret_cast<const float*>(s)[e];
+    else return __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(s)[e]);
+  }
 };
 
-template <int G> __device__ __forceinline__ void group_sync() {
-  if constexpr (G == 32) __syncwarp();
-  else __syncthreads();
-}
-
-// Sums with the maximum known: s = sum e, t = sum e d, e = 2^d, d = (x - m) log2(e) / tau = (x - m) c.
-//   Near: d is taken as x c - mc in one operation, mc = m c rounded.  That rounding (the slip, known exactly from another fused operation) moves all
-//   exponents of the row alike, so sums can be put right at the end, and it is small where |m c| is; that saves half an instruction per
-//   logit.  Rows farther from 0 (or masked with -1e9, or with the type's lowest value) take the difference first.
-constexpr float kNear = 4096.f;        // |m c| below which the slip is below 2^-12
-struct Sums { float s, t; };
+// ---- exponents ---------------------------------------------------------------------------------------------------------------
+// e = 2^d, d = (x - m) c, c = log2(e) / tau.  Near 0 (|m c| < 2^21) d is taken as x c - R in one operation, R the whole number next to m c (or to that of an
+// earlier maximum): R is exact, so all of a row's exponents are off by the one number m c - R, by which the sums are put right (delta).  That saves
+// half an instruction per logit.  Far from 0, where x c has no fraction left (masks of -1e9, of the type's lowest value), the difference is taken first.
+constexpr float kFar = 2097152.f;      // 2^21
+__device__ __forceinline__ float safe_max(float m) { return m == -INFINITY ? 0.f : m; }
+__device__ __forceinline__ bool is_near(float m, float c) { return fabsf(m * c) < kFar; }
+__device__ __forceinline__ float whole_ref(float m, float c) { return fmaxf(rintf(m * c), -2.f * kFar); }   // a thread far below the row's maximum adds nothing
+__device__ __forceinline__ float delta(float m, float c, float R) { return fmaf(-m, c, R); }   // d from m less d from R
 template <bool NEAR> struct Expo {
   uint64_t a, b;
-  __device__ __forceinline__ Expo(float m, float c) : a(pack2(c, c)), b(NEAR ? pack2(-(m * c), -(m * c)) : pack2(-m, -m)) {}
+  __device__ __forceinline__ Expo(float ref, float c) : a(pack2(c, c)), b(pack2(-ref, -ref)) {}   // ref: R near, m far
   __device__ __forceinline__ uint64_t operator()(uint64_t x) const { return NEAR ? fma2(x, a, b) : mul2(add2(x, b), a); }
-  static __device__ __forceinline__ float slip(float m, float c) { return NEAR ? fmaf(m, c, -(m * c)) : 0.f; }   // d comes out too large by this
 };
 __device__ __forceinline__ uint64_t exp2_pair(uint64_t d) {
   float a, b;
   unpack2(d, a, b);
   return pack2(exp2_fast(a), exp2_fast(b));
 }
-template <typename T, int G, bool ENT, bool NEAR> __device__ __forceinline__ Sums thread_sums(const Slice<T, G>& sl, float m, float c) {
-  constexpr int P = Elem<T>::E / 2;
-  const Expo<NEAR> ex(m, c);
+__device__ __forceinline__ float sum_pair(uint64_t v) {
+  float a, b;
+  unpack2(v, a, b);
+  return a + b;
+}
+// s = sum e and t = sum e d over vectors of logits.
+template <typename T, bool ENT> struct Sums {
   uint64_t s[2] = {0, 0}, t[2] = {0, 0};
-  sl.each([&](const uint4& u) {
+  template <typename X> __device__ __forceinline__ void add(const uint4& u, const X& ex) {
+    constexpr int P = Elem<T>::E / 2;
     uint64_t x[P];
     Elem<T>::unpack(u, x);
 #pragma unroll
     for (int i = 0; i < P; ++i) {
       const uint64_t d = ex(x[i]), e = exp2_pair(d);
       s[i & 1] = add2(s[i & 1], e);
-      if (ENT) t[i & 1] = fma2(e, d, t[i & 1]);
-    }
-  });
-  Sums r{0.f, 0.f};
-  float a, b;
-  unpack2(add2(s[0], s[1]), a, b);
-  r.s = a + b;
-  if (ENT) {
-    unpack2(add2(t[0], t[1]), a, b);
-    r.t = a + b;
-    if (r.t != r.t && r.s == r.s) {     // 0 * -inf: the thread has met logits of -inf, which add nothing
-      t[0] = 0;
-      sl.each([&](const uint4& u) {
-        uint64_t x[P];
-        Elem<T>::unpack(u, x);
-#pragma unroll
-        for (int i = 0; i < P; ++i) {
-          const uint64_t d = ex(x[i]);
-          unpack2(d, a, b);
-          t[0] = fma2(exp2_pair(d), pack2(fmaxf(a, -1e30f), fmaxf(b, -1e30f)), t[0]);
-        }
-      });
-      unpack2(t[0], a, b);
-      r.t = a + b;
+      if (ENT) {
+        float a, b;
+        unpack2(d, a, b);
+        t[i & 1] = fma2(e, pack2(fmaxf(a, -1e30f), fmaxf(b, -1e30f)), t[i & 1]);   // a logit of -inf adds 0, not 0 * -inf
+      }
     }
   }
-  return r;
-}
-__device__ __forceinline__ bool is_near(float m, float c) { return fabsf(m * c) < kNear; }
+};
 
 // What the parts of a row know of it, and what the whole row comes to.
 struct Part { float m, s, t; };
 struct Stat { float m, L, H, s; };
-__device__ __forceinline__ float safe_max(float m) { return m == -INFINITY ? 0.f : m; }
+// Sums whose exponents were too small by delta, against m.
+template <typename S> __device__ __forceinline__ Part part_of(float m, const S& sums, float delta) {
+  const float s = sum_pair(add2(sums.s[0], sums.s[1])), t = sum_pair(add2(sums.t[0], sums.t[1]));
+  if (s == 0.f) return {m, 0.f, 0.f};
+  const float f = exp2_fast(delta);
+  return {m, s * f, fmaf(delta, s, t) * f};
+}
 template <bool ENT> __device__ __forceinline__ Stat stat_of(float m, float s, float t) {
+  if (s > 0.f && s < 1.f) s = 1.f;      // rounding: the largest logit alone adds 1, and no log probability is above 0
   Stat r{m, logf(s), 0.f, s};
-  if (ENT && s != 0.f) r.H = r.L - kLn2 * (t / s);
+  if (ENT && s != 0.f) {
+    r.H = r.L - kLn2 * (t / s);
+    if (r.H < 0.f) r.H = 0.f;
+  }
   return r;
 }
-// The whole row from its parts (at most 8), by a whole warp: a part's exponents were taken against its own maximum.
-template <bool ENT> __device__ __forceinline__ Stat stat_of_parts(const Part* parts, int n, float c, int lane) {
-  Part p{-INFINITY, 0.f, 0.f};
-  if (lane < n) p = parts[lane];
-  const float m = warp_max(p.m);
-  const float up = (safe_max(p.m) - safe_max(m)) * c, f = p.s == 0.f ? 0.f : exp2_fast(up);   // s = 0: nothing but -inf, its up means nothing
-  float s = p.s * f, t = ENT && f != 0.f ? fmaf(p.s, up, p.t) * f : 0.f;
-#pragma unroll
-  for (int o = kMaxCluster / 2; o > 0; o >>= 1) {
-    s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
-    if (ENT) t += __shfl_xor_sync(0xFFFFFFFFu, t, o);
-  }
-  s = __shfl_sync(0xFFFFFFFFu, s, 0);
-  if (ENT) t = __shfl_sync(0xFFFFFFFFu, t, 0);
-  return stat_of<ENT>(m, s, t);
+// Two sets of elements, each with its sums against its own maximum, against a common one.  s = 0: nothing but -inf, its maximum means nothing.
+template <bool ENT> __device__ __forceinline__ Part against(const Part& p, float m, float c) {
+  const float up = (safe_max(p.m) - safe_max(m)) * c, f = p.s == 0.f ? 0.f : exp2_fast(up);
+  return {m, p.s * f, ENT && f != 0.f ? fmaf(p.s, up, p.t) * f : 0.f};
 }
-
-// The row's copy has arrived.  A wait that runs out is reported; it is waited for once more, so that no copy lands after the kernel.
-__device__ __forceinline__ void row_wait(uint64_t* bar, int32_t* status) {
-  if (mbar_wait(bar, 0)) return;
-  put_status(status, DEV_TIMEOUT_TMA);
-  mbar_wait(bar, 0);
-}
-
-// ---- scratch of a group beside its slice ---------------------------------------------------------------------------------
-constexpr int kFewAlt = 24;        // up to here the alternatives are bounded by the maxima of 32 groups of threads, beyond by those of 128
-constexpr int kThreadGroups = 128;
-template <int G, bool ALT> struct alignas(16) Scratch {
-  static constexpr int kCand = !ALT ? 0 : G == 32 ? 256 : 1024;
-  float gm[ALT && G > 32 ? kThreadGroups : 4];
-  float2 red[G / 32];
-  float red_m[G / 32];
-  float m, thr;
-  int count;
-  unsigned long long bar;
-  Part part[kMaxCluster];
-  unsigned long long best[ALT ? G / 32 : 1];
-  unsigned long long list[ALT ? kMaxAlt : 1];
-  unsigned long long peers[ALT && G > 32 ? kMaxCluster * kMaxAlt : 1];   // the lists of the cluster's CTAs, in the first of them
-  unsigned long long cand[kCand > 0 ? kCand : 1];
-};
-
-// The maximum of the group's part of the row, in every thread.
-template <typename T, int G, bool ALT> __device__ __forceinline__ float part_max(const Slice<T, G>& sl, Scratch<G, ALT>& sc, float mine) {
-  float m = warp_max(mine);
-  if constexpr (G > 32) {
-    if ((sl.t & 31) == 0) sc.red_m[sl.t >> 5] = m;
-    __syncthreads();
-    m = sc.red_m[0];
-#pragma unroll
-    for (int w = 1; w < G / 32; ++w) m = fmaxf(m, sc.red_m[w]);
-  }
-  return m;
-}
-// The warp's values in descending order of the lanes (a bitonic network).
-__device__ __forceinline__ float sort_descending(float v, int lane) {
-#pragma unroll
-  for (int k = 2; k <= 32; k *= 2)
-#pragma unroll
-    for (int j = k / 2; j > 0; j /= 2) {
-      const float o = __shfl_xor_sync(0xFFFFFFFFu, v, j);
-      v = ((lane & j) == 0) == ((lane & k) == 0) ? fmaxf(v, o) : fminf(v, o);
-    }
-  return v;
-}
-// The maximum, and a value that at least n_alt of the part's elements reach: the n_alt-th largest among the maxima of groups of threads.  Where large
-// values are spread over the row, 1.2 n_alt elements reach that of 128 groups at n_alt 64, 1.8 n_alt that of 32 at 24 (of 24 at 24: 3.8 n_alt).  kLowest where fewer
-// groups have a value.
-template <typename T, int G> __device__ __forceinline__ float part_max_and_threshold(const Slice<T, G>& sl, Scratch<G, true>& sc, float mine, int n_alt, float& thr) {
-  float m;
-  const int lane = sl.t & 31;
-  if (G == 32 || n_alt <= kFewAlt) {
-    float g = mine;
-    if constexpr (G > 32) {
-      constexpr int SG = G / 32;
-#pragma unroll
-      for (int o = SG / 2; o > 0; o >>= 1) g = fmaxf(g, __shfl_xor_sync(0xFFFFFFFFu, g, o));
-      if (sl.t % SG == 0) sc.gm[sl.t / SG] = g;
-      __syncthreads();
-      g = sc.gm[lane];
-    }
-    g = sort_descending(g, lane);
-    m = __shfl_sync(0xFFFFFFFFu, g, 0);
-    thr = __shfl_sync(0xFFFFFFFFu, g, n_alt - 1);
-  } else if constexpr (G > 32) {
-    constexpr int SG = G / kThreadGroups;
-    float g = mine;
-#pragma unroll
-    for (int o = SG / 2; o > 0; o >>= 1) g = fmaxf(g, __shfl_xor_sync(0xFFFFFFFFu, g, o));
-    if (sl.t % SG == 0) sc.gm[sl.t / SG] = g;
-    __syncthreads();
-    if (sl.t < kThreadGroups) {
-      const float my = sc.gm[sl.t];
-      int rank = 0;
-#pragma unroll 8
-      for (int j = 0; j < kThreadGroups; j += 4) {
-        const float4 v = *reinterpret_cast<const float4*>(sc.gm + j);
-        rank += (v.x > my || (v.x == my && j < sl.t)) + (v.y > my || (v.y == my && j + 1 < sl.t)) + (v.z > my || (v.z == my && j + 2 < sl.t)) +
-                (v.w > my || (v.w == my && j + 3 < sl.t));
-      }
-      if (rank == 0) sc.m = my;
-      if (rank == n_alt - 1) sc.thr = my;
-    }
-    __syncthreads();
-    m = sc.m;
-    thr = sc.thr;
-  }
-  thr = fmaxf(thr, Elem<T>::kLowest);     // -inf is never an alternative
-  return m;
-}
-
-// The sums of the group's part against m, in every thread.
-template <bool ENT, typename T, int G, bool ALT> __device__ __forceinline__ Sums part_sums(const Slice<T, G>& sl, Scratch<G, ALT>& sc, float m, float c) {
-  const bool near = is_near(m, c);
-  Sums r = near ? thread_sums<T, G, ENT, true>(sl, m, c) : thread_sums<T, G, ENT, false>(sl, m, c);
+// The union of a warp's sets, in every lane.
+template <bool ENT> __device__ __forceinline__ Part warp_union(const Part& mine, float c) {
+  Part r = against<ENT>(mine, warp_max(mine.m), c);
   r.s = warp_sum(r.s);
   if (ENT) r.t = warp_sum(r.t);
-  if constexpr (G > 32) {
-    if ((sl.t & 31) == 0) sc.red[sl.t >> 5] = make_float2(r.s, r.t);
-    __syncthreads();
-    r = {0.f, 0.f};
-#pragma unroll
-    for (int w = 0; w < G / 32; ++w) { r.s += sc.red[w].x; r.t += sc.red[w].y; }
-  } else {
-    __syncwarp();
-  }
-  if (near) {
-    const float slip = Expo<true>::slip(m, c), f = fmaf(-kLn2, slip, 1.f);   // 2^-slip
-    if (ENT) r.t = fmaf(-slip, r.s, r.t) * f;
-    r.s *= f;
-  }
   return r;
 }
-
-template <typename T> __device__ __forceinline__ float slice_elem(const uint4* s, int v, int e) {
-  if constexpr (sizeof(T) == 4) return reinterpret_cast<const float*>(s + v)[e];
-  else return __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(s + v)[e]);
-}
-
-// The keys of the part's elements that reach the threshold, in any order.  Few threads hold one; a warp goes over the vectors of each such thread together.
-template <typename T, int G> __device__ __forceinline__ void part_candidates(const Slice<T, G>& sl, Scratch<G, true>& sc, float mine, float thr) {
-  const int lane = sl.t & 31;
-  for (uint32_t who = __ballot_sync(0xFFFFFFFFu, mine >= thr); who; who &= who - 1) {
-    for (int v = (sl.t & ~31) + __ffs(who) - 1 + lane * G; v < sl.n; v += 32 * G) {
-      const uint4 u = sl.s[v];
-      uint64_t x[Elem<T>::E / 2];
-      Elem<T>::unpack(u, x);
-      const int i0 = sl.first_index(v);
-#pragma unroll
-      for (int e = 0; e < Elem<T>::E; ++e) {
-        float a, b;
-        unpack2(x[e >> 1], a, b);
-        const float f = e & 1 ? b : a;
-        if (f >= thr) {
-          const int slot = atomicAdd(&sc.count, 1);
-          if (slot < Scratch<G, true>::kCand) sc.cand[slot] = alt_key(f, i0 + e);
-        }
-      }
-    }
+// The whole row from its parts, one of each warp that went over it (at most 64), by a whole warp.
+template <bool ENT> __device__ __forceinline__ Stat stat_of_parts(const Part* parts, int n, float c, int lane) {
+  Part p{-INFINITY, 0.f, 0.f};
+  if (lane < n) p = {parts[lane].m, parts[lane].s, ENT ? parts[lane].t : 0.f};
+  if (n > 32) {
+    Part q{-INFINITY, 0.f, 0.f};
+    if (lane + 32 < n) q = {parts[lane + 32].m, parts[lane + 32].s, ENT ? parts[lane + 32].t : 0.f};
+    const float m = fmaxf(p.m, q.m);
+    p = against<ENT>(p, m, c);
+    q = against<ENT>(q, m, c);
+    p.s += q.s;
+    p.t += q.t;
   }
-  group_sync<G>();
+  p = warp_union<ENT>(p, c);
+  return stat_of<ENT>(p.m, p.s, p.t);
 }
 
-// list[0 ... n_alt): the keys of the part's largest elements in descending order, 0 where there are fewer.  From the elements that reached the
-// threshold, each ranked by counting; where there were too many to keep (rows of mostly equal values), by n_alt searches for the next largest key.
-template <typename T, int G> __device__ __forceinline__ void part_list(const Slice<T, G>& sl, Scratch<G, true>& sc, int n_alt) {
-  const int c = sc.count;
-  if (c <= Scratch<G, true>::kCand) {
-    for (int i = sl.t; i < c; i += G) {
-      const unsigned long long key = sc.cand[i];
-      int rank = 0;
-      for (int j = 0; j < c; ++j) rank += sc.cand[j] > key;
-      if (rank < n_alt) sc.list[rank] = key;
-    }
-  } else {
-    unsigned long long prev = ~0ull;
-    for (int a = 0; a < n_alt; ++a) {
-      unsigned long long best = 0;
-      for (int v = sl.t; v < sl.n; v += G) {
-        const int i0 = sl.first_index(v);
-#pragma unroll
-        for (int e = 0; e < Elem<T>::E; ++e) {
-          const float x = slice_elem<T>(sl.s, v, e);
-          const unsigned long long key = x >= Elem<T>::kLowest ? alt_key(x, i0 + e) : 0;
-          if (key < prev && key > best) best = key;
-        }
-      }
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) {
-        const unsigned long long other = __shfl_xor_sync(0xFFFFFFFFu, best, o);
-        best = other > best ? other : best;
-      }
-      if constexpr (G > 32) {
-        if ((sl.t & 31) == 0) sc.best[sl.t >> 5] = best;
-        __syncthreads();
-#pragma unroll
-        for (int w = 0; w < G / 32; ++w) best = sc.best[w] > best ? sc.best[w] : best;
-        __syncthreads();
-      }
-      if (sl.t == 0) sc.list[a] = best;
-      prev = best;
-      if (best == 0) break;
-    }
-  }
-  group_sync<G>();
-}
-
-// ---- log probabilities of given tokens, statistics, entropy, alternatives ------------------------------------------------
 struct RowsArgs {
-  const void* x; long long ld; int rows, V, per_max, lg;   // per_max: vectors of the largest slice; lg: of the CTAs that share a row, the logarithm
+  const void* x; long long ld; int rows, V;
+  int per_max, lg;    // vectors of the largest part of a row; log2 of the CTAs that share one
   float inv_tau;
-  const int32_t* ids; int n_alt;
-  float* logprob; float2* stats; float* entropy; int32_t* alt_ids; float* alt_logprob;
   int32_t* status;
 };
 
-constexpr int kWarpRows = 2;       // rows of a CTA where a warp takes one
-template <int G> constexpr int cta_threads() { return G == 32 ? 32 * kWarpRows : G; }
-template <typename S> __host__ __device__ constexpr size_t group_bytes(int per_max) { return (size_t)per_max * 16 + sizeof(S); }
+// ---- rows that are read once: a stream through the registers ---------------------------------------------------------------
+// A warp (G 32) or the four warps of a CTA (G 128; in a cluster each CTA has a part of the row) go over a row.  Thread t reads the whole
+// vectors t, t + G, ... of its part, in blocks of four, and keeps a running maximum beside sums against a reference that changes only where
+// the maximum passes it by 2^64.  The blocks come through a ring in shared memory in which every lane has its own slots: copies of
+// kAhead blocks are on their way while one is summed, which in registers would cost half of the warps.  Nothing of the row is kept; what holds
+// the alternatives is read again, from L2.
+constexpr int kStreamThreads = 128, kStreamWarps = 4, kBlock = 4, kAhead = 2;
+constexpr int kRingBytes = (kAhead + 1) * kBlock * 32 * 16;   // of a warp
+constexpr int kMaxWarps = kMaxCluster * kStreamWarps;   // warps that share a row
+
+template <typename T, int G> struct Stream {
+  static constexpr int E = Elem<T>::E, B = kBlock;
+  const T* row;      // first logit of the row
+  int off, V, v0;    // elements between the 16-byte boundary and the row; logits of the row; first vector of this part
+  int t, nw, part;   // thread of the group; whole vectors of the part; the partial vector that this thread has beside, or -1
+  const char* base;  // the part's first whole vector
+  __device__ __forceinline__ Stream(const T* row_, int V_, int rank, int lg_parts, int t_) : row(row_), V(V_), t(t_) {
+    off = (int)((reinterpret_cast<uintptr_t>(row) & 15u) / sizeof(T));
+    const int nv = (off + V + E - 1) / E, b = nv >> lg_parts, rem = nv & ((1 << lg_parts) - 1);
+    const int n = b + (rank < rem), v = rank * b + min(rank, rem);
+    const bool head = v == 0 && off > 0 && n > 0, tail = n > 0 && v + n == nv && (off + V) % E && !(head && n == 1);
+    part = head && t == 0 ? 0 : tail && t == G - 1 ? nv - 1 : -1;
+    v0 = v + head;
+    nw = n - head - tail;
+    base = reinterpret_cast<const char*>(row - off) + (size_t)v0 * 16;
+  }
+  __device__ __forceinline__ int turns() const { return (nw + B * G - 1) / (B * G); }   // blocks of the thread that has most
+  __device__ __forceinline__ uint4 load(int j) const { return dep_load16(base + (size_t)j * 16); }
+  __device__ __forceinline__ int index_of(int j) const { return (v0 + j) * E - off; }   // logit that whole vector j starts with
+  __device__ __forceinline__ uint4 partial() const {            // its elements that are not the row's are -inf
+    float x[E];
+    const int i0 = part * E - off;
+#pragma unroll
+    for (int e = 0; e < E; ++e) x[e] = Elem<T>::load(row + min(max(i0 + e, 0), V - 1));
+    uint64_t f[E / 2];
+#pragma unroll
+    for (int e = 0; e < E; e += 2)
+      f[e / 2] = pack2(i0 + e >= 0 && i0 + e < V ? x[e] : -INFINITY, i0 + e + 1 >= 0 && i0 + e + 1 < V ? x[e + 1] : -INFINITY);
+    return Elem<T>::pack(f);
+  }
+  // f(vectors, how many, block) for the thread's blocks of up to B vectors, the partial one last and alone (block -1).  ring: the warp's.
+  template <typename F> __device__ __forceinline__ void each(uint4* ring, F f) const {
+    const uint32_t slot = smem_u32(ring + (t & 31));
+    const char* g = base + (size_t)t * 16;
+    int left = nw - t, next = left;              // vectors times G that are not summed, not asked for
+    const auto ask = [&](int s) {
+#pragma unroll
+      for (int i = 0; i < B; ++i)
+        if (next > i * G) cp_async16(slot + (s * B + i) * 512, g + (size_t)i * G * 16);
+      asm volatile("cp.async.commit_group;" ::: "memory");
+      next -= B * G;
+      g += (size_t)B * G * 16;
+    };
+#pragma unroll
+    for (int s = 0; s < kAhead; ++s) ask(s);
+    int k = 0;
+    for (int s = 0; left > 0; ++k, left -= B * G, s = s == kAhead ? 0 : s + 1) {
+      ask(s == 0 ? kAhead : s - 1);              // into the block before this one, which the lane has read
+      asm volatile("cp.async.wait_group %0;" ::"n"(kAhead) : "memory");
+      const uint4* mine = ring + s * B * 32 + (t & 31);
+      if (left > (B - 1) * G) {
+        uint4 a[B];
+#pragma unroll
+        for (int i = 0; i < B; ++i) a[i] = mine[i * 32];
+        f(a, std::integral_constant<int, B>(), k);
+      } else {
+        for (int i = 0; left > i * G; ++i) f(mine + i * 32, std::integral_constant<int, 1>(), k);
+      }
+    }
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    if (part >= 0) {
+      const uint4 a = partial();
+      f(&a, std::integral_constant<int, 1>(), -1);
+    }
+  }
+};
+
+// The running state of a thread.
+template <typename T, bool ENT> struct Online {
+  float c, m = -INFINITY, R = 0.f, limit = -INFINITY;   // limit: largest maximum that the reference bears
+  Sums<T, ENT> sums;
+  __device__ __forceinline__ explicit Online(float c_) : c(c_) {}
+  template <int N> __device__ __forceinline__ float add(const uint4* u) {   // the vectors' maximum
+    typename Elem<T>::Max mx;
+#pragma unroll
+    for (int i = 0; i < N; ++i) mx.add(u[i]);
+    const float bm = mx.value();
+    m = fmaxf(m, bm);
+    if (bm > limit) {
+      const float to = whole_ref(bm, c);
+      if (limit != -INFINITY) {
+        const float d = R - to, f = exp2_fast(d);
+        const uint64_t d2 = pack2(d, d), f2 = pack2(f, f);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          if (ENT) sums.t[i] = mul2(fma2(sums.s[i], d2, sums.t[i]), f2);
+          sums.s[i] = mul2(sums.s[i], f2);
+        }
+      }
+      R = to;
+      limit = bm + 64.f / c;
+    }
+    const Expo<true> ex(R, c);
+#pragma unroll
+    for (int i = 0; i < N; ++i) sums.add(u[i], ex);
+    return bm;
+  }
+  __device__ __forceinline__ Part part() const { return part_of(m, sums, delta(safe_max(m), c, R)); }
+};
+// A row whose maximum m is far from 0: the sums once more, against it.
+template <typename T, int G, bool ENT> __device__ __forceinline__ Part far_part(const Stream<T, G>& st, uint4* ring, float m, float c) {
+  Sums<T, ENT> sums;
+  const Expo<false> ex(m, c);
+  st.each(ring, [&](const uint4* u, auto n, int) {
+#pragma unroll
+    for (int i = 0; i < decltype(n)::value; ++i) sums.add(u[i], ex);
+  });
+  return part_of(m, sums, 0.f);
+}
+
+// ---- alternatives --------------------------------------------------------------------------------------------------------
+constexpr int kFewAlt = 24;        // up to here they are bounded by the maxima of 32 groups of threads, beyond by those of 128
+constexpr int kThreadGroups = 128;
+constexpr int kMaxCand = 256;      // elements that a warp can keep
+struct alignas(16) WarpAlt {
+  unsigned long long cand[kMaxCand];
+  float gm[32];
+  uint16_t hit[kMaxCand];
+};
+static_assert(sizeof(WarpAlt) <= kRingBytes, "takes the ring's place");
+struct alignas(16) RowAlt {        // of a row that warps share (in every CTA of a cluster)
+  float own[kThreadGroups], all[kThreadGroups];   // maxima of groups of threads, of this CTA and of the cluster
+  float bound[kMaxCluster];        // what the cluster's CTAs found on their own
+  float nth;
+  int count[kMaxWarps];            // of the warps' lists, which lie behind this: [warps][n_alt], in the cluster's first CTA
+};
+
+__device__ __forceinline__ int rank_among(float my, int i, const float* gm, int n) {   // how many of gm are larger, or equal and in front of i
+  int rank = 0;
+#pragma unroll 8
+  for (int j = 0; j < n; j += 4) {
+    const float4 v = *reinterpret_cast<const float4*>(gm + j);
+    rank += (v.x > my || (v.x == my && j < i)) + (v.y > my || (v.y == my && j + 1 < i)) + (v.z > my || (v.z == my && j + 2 < i)) + (v.w > my || (v.w == my && j + 3 < i));
+  }
+  return rank;
+}
+// The n-th largest of the maxima of 32 groups of threads: at least n of the elements that they went over reach it, about n (1 + n / 40) where large
+// values are spread over them.  Every warp for itself.
+__device__ __forceinline__ float nth_of_32(const float* gm, int n, int lane) {
+  const float my = gm[lane];
+  const uint32_t who = __ballot_sync(0xFFFFFFFFu, rank_among(my, lane, gm, 32) == n - 1);
+  return __shfl_sync(0xFFFFFFFFu, my, __ffs(who) - 1);
+}
+// The same of 128 groups (1.2 n elements at n 64), by the CTA.
+__device__ __forceinline__ float nth_of_128(const float* gm, float* out, int n) {
+  const float my = gm[threadIdx.x];
+  if (rank_among(my, threadIdx.x, gm, kThreadGroups) == n - 1) *out = my;
+  __syncthreads();
+  const float r = *out;
+  __syncthreads();
+  return r;
+}
+// The largest of v over groups of 32 / per neighbouring lanes (per a power of two), in each of their lanes.
+__device__ __forceinline__ float lane_group_max(float v, int per) {
+  for (int o = 16 / per; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xFFFFFFFFu, v, o));
+  return v;
+}
+
+// What a warp has found: keys in no order, all of them larger than what it has left out.
+struct Found {
+  unsigned long long* key;   // [kMaxCand]
+  int n, lane;
+  unsigned long long floor;  // smallest key worth keeping
+  // Every lane brings some elements of a vector (a bit each).  False where they do not fit.
+  template <typename T> __device__ __forceinline__ bool add(const uint4& u, uint32_t bits, int index) {
+    for (uint32_t who; (who = __ballot_sync(0xFFFFFFFFu, bits != 0)) != 0;) {
+      if (n + __popc(who) > kMaxCand) return false;
+      if (bits) {
+        const int e = __ffs(bits) - 1;
+        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+        uint32_t word = w[0];
+#pragma unroll
+        for (int i = 1; i < 4; ++i) word = (sizeof(T) == 4 ? e : e >> 1) == i ? w[i] : word;
+        const float f = sizeof(T) == 4 ? __uint_as_float(word) : __uint_as_float(e & 1 ? word & 0xFFFF0000u : word << 16);
+        key[n + __popc(who & ((1u << lane) - 1))] = alt_key(f, index + e);
+        bits &= bits - 1;
+      }
+      n += __popc(who);
+    }
+    return true;
+  }
+  // Down to the `most` largest, in descending order.
+  __device__ __forceinline__ void cut(int most) {
+    __syncwarp();
+    unsigned long long k[kMaxCand / 32];
+    int place[kMaxCand / 32];
+#pragma unroll
+    for (int i = 0; i < kMaxCand / 32; ++i) {
+      place[i] = kMaxCand;
+      if (32 * i >= n) continue;
+      k[i] = lane + 32 * i < n ? key[lane + 32 * i] : 0;
+      if (lane + 32 * i < n) place[i] = 0;
+#pragma unroll 4
+      for (int j = 0; j < n; ++j) place[i] += key[j] > k[i];
+    }
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < kMaxCand / 32; ++i)
+      if (place[i] < most) key[place[i]] = k[i];
+    __syncwarp();
+    n = min(n, most);
+    if (n == most) floor = key[n - 1] + 1;
+  }
+};
+template <typename T> __device__ __forceinline__ uint32_t reach_bits(const uint4& u, float thr) {   // elements of at least thr
+  constexpr int E = Elem<T>::E;
+  typename Elem<T>::Max mx;
+  mx.add(u);
+  if (!(mx.value() >= thr)) return 0;
+  uint64_t x[E / 2];
+  Elem<T>::unpack(u, x);
+  uint32_t bits = 0;
+#pragma unroll
+  for (int e = 0; e < E; e += 2) {
+    float a, b;
+    unpack2(x[e / 2], a, b);
+    bits |= (a >= thr ? 1u << e : 0u) | (b >= thr ? 2u << e : 0u);
+  }
+  return bits;
+}
+
+// The warp's elements that reach thr, at most most of them where there are many.  bm: [turns][32] maxima of the lanes' blocks.  A few blocks hold one: their vectors
+// are read again, spread over the warp.  Where they are too many (rows of mostly equal values, rows in order), the warp goes over all of its
+// vectors once more and keeps the largest `most` of what it has met whenever it runs out of room.
+template <typename T, int G> __device__ __forceinline__ void warp_select(const Stream<T, G>& st, const float* bm, float partial_max, float thr, int most, WarpAlt& wa, Found& f) {
+  constexpr int B = Stream<T, G>::B;
+  const int lane = st.t & 31, turns = st.turns();
+  const uint32_t below = (1u << lane) - 1;
+  f.key = wa.cand;
+  f.lane = lane;
+  f.n = 0;
+  f.floor = 1;
+  uint4 u{};
+  const uint32_t mine = st.part >= 0 && partial_max >= thr;
+  if (__any_sync(0xFFFFFFFFu, mine)) {
+    if (mine) u = st.partial();
+    f.add<T>(u, mine ? reach_bits<T>(u, thr) : 0, st.part * Elem<T>::E - st.off);
+  }
+  int h = 0;
+  for (int k = 0; k < turns; ++k) {
+    const bool hit = bm[k * 32 + lane] >= thr;
+    const uint32_t who = __ballot_sync(0xFFFFFFFFu, hit);
+    const int at = h + __popc(who & below);
+    if (hit && at < kMaxCand) wa.hit[at] = (uint16_t)(k * 32 + lane);
+    h += __popc(who);
+  }
+  __syncwarp();
+  bool fits = h <= kMaxCand;
+  const int t0 = st.t - lane;
+  for (int q0 = 0; fits && q0 < B * h; q0 += 128) {
+    uint4 v[4];
+    int j[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int q = q0 + 32 * i + lane;
+      j[i] = st.nw;
+      if (q < B * h) {
+        const int code = wa.hit[q / B];
+        j[i] = t0 + (code & 31) + ((code >> 5) * B + q % B) * G;
+      }
+      if (j[i] < st.nw) v[i] = st.load(j[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (fits) fits = f.add<T>(v[i], j[i] < st.nw ? reach_bits<T>(v[i], thr) : 0, st.index_of(j[i]));
+  }
+  if (fits) {
+    __syncwarp();
+    return;
+  }
+  f.n = 0;
+  const auto over = [&](const uint4& x, uint32_t bits, int index) {
+    uint32_t rest = bits;
+    while (__any_sync(0xFFFFFFFFu, rest != 0)) {       // one element of each lane at a time
+      const uint32_t low = rest & -rest;
+      if (f.n > kMaxCand - 32) f.cut(most);
+      uint32_t take = low;
+      if (low) {                                       // what is below the kept ones is left out
+        const int e = __ffs(low) - 1;
+        uint64_t p[Elem<T>::E / 2];
+        Elem<T>::unpack(x, p);
+        float v = 0.f;
+#pragma unroll
+        for (int i = 0; i < Elem<T>::E; ++i) {
+          float a, b;
+          unpack2(p[i / 2], a, b);
+          if (i == e) v = i & 1 ? b : a;
+        }
+        if (alt_key(v, index + e) < f.floor) take = 0;
+      }
+      f.add<T>(x, take, index);
+      rest &= ~low;
+    }
+  };
+  if (__any_sync(0xFFFFFFFFu, mine)) over(u, mine ? reach_bits<T>(u, thr) : 0, st.part * Elem<T>::E - st.off);
+  for (int q = 0; q < turns * B; ++q) {
+    if (!__any_sync(0xFFFFFFFFu, bm[q / B * 32 + lane] >= thr)) continue;
+    const int j = st.t + q * G;
+    uint4 x{};
+    if (j < st.nw) x = st.load(j);
+    over(x, j < st.nw ? reach_bits<T>(x, thr) : 0, st.index_of(j));
+  }
+  f.cut(most);
+}
+
+// ---- log probabilities of given tokens, statistics, entropy, alternatives ------------------------------------------------
+struct TokenArgs {
+  RowsArgs r;
+  const int32_t* ids; int n_alt, turns;     // turns: blocks of the thread that has most
+  float* logprob; float2* stats; float* entropy; int32_t* alt_ids; float* alt_logprob;
+};
+// The scratch of a row that warps share: what each of them has found, and what it finds where the row has to be gone over again.
+struct alignas(16) Shared { Part part[2][kMaxWarps]; };
+// Every CTA of the cluster has every warp's part, behind a barrier of all threads that share the row.
+template <bool ENT> __device__ __forceinline__ void share_parts(Shared& sh, const Part& part, int turn, int parts, int rank, int warp, int lane) {
+  if (lane < parts) {
+    const uint32_t to = peer_smem(&sh.part[turn][rank * kStreamWarps + warp], lane);
+    peer_store(to, part.m); peer_store(to + 4, part.s);
+    if (ENT) peer_store(to + 8, part.t);
+  }
+  __syncwarp();
+  if (parts > 1) cluster_sync_all();
+  else __syncthreads();
+}
+
+template <bool ENT> __device__ __forceinline__ void tell_alt(const TokenArgs& p, int row, const Stat& st, int place, unsigned long long key) {   // key 0: none
+  const bool bad = st.L != st.L;
+  p.alt_ids[(size_t)row * p.n_alt + place] = bad || !key ? -1 : alt_index(key);
+  p.alt_logprob[(size_t)row * p.n_alt + place] = bad ? st.L : key ? (alt_value(key) - st.m) * p.r.inv_tau - st.L : -INFINITY;
+}
+template <typename T, bool ENT> __device__ __forceinline__ void tell_row(const TokenArgs& p, int row, const Stat& st, int id, float xid) {
+  if (p.stats) p.stats[row] = make_float2(st.m, st.L);
+  if (ENT) p.entropy[row] = st.H;
+  if (!p.logprob) return;
+  float lp = 0.f;                      // -1: the row has no token
+  if (id >= 0 && id < p.r.V) {
+    lp = st.L == -INFINITY ? -INFINITY : (xid - st.m) * p.r.inv_tau - st.L;
+  } else if (id != -1) {
+    put_status(p.r.status, DEV_BAD_TOKEN_ID);
+    lp = __int_as_float(0x7FC00000);
+  }
+  p.logprob[row] = lp;
+}
 
 template <typename T, int G, bool ENT, bool ALT>
-__global__ void __launch_bounds__(cta_threads<G>()) token_logprobs_kernel(const RowsArgs p) {
-  using S = Scratch<G, ALT>;
+__global__ void __launch_bounds__(kStreamThreads, 8) token_logprobs_kernel(const TokenArgs p) {
+  constexpr int W = kStreamWarps;
   extern __shared__ uint4 smem[];
   pdl_trigger();
-  const int parts = G == 32 ? 1 : 1 << p.lg, rank = G == 32 ? 0 : (int)cluster_ctarank();
-  const int sub = G == 32 ? threadIdx.x >> 5 : 0, t = G == 32 ? threadIdx.x & 31 : threadIdx.x;
-  const int row = G == 32 ? blockIdx.x * kWarpRows + sub : blockIdx.x >> p.lg;
+  const int parts = G == 32 ? 1 : 1 << p.r.lg, rank = parts > 1 ? (int)cluster_ctarank() : 0, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int row = G == 32 ? blockIdx.x * W + warp : blockIdx.x >> p.r.lg;
+  if (parts > 1) cluster_arrive_relaxed();
   pdl_wait();
-  if (G == 32 && row >= p.rows) return;
-  if (G > 32 && parts > 1) cluster_arrive_relaxed();
-  uint4* mine = reinterpret_cast<uint4*>(reinterpret_cast<char*>(smem) + sub * group_bytes<S>(p.per_max));
-  S& sc = *reinterpret_cast<S*>(mine + p.per_max);
-  const T* xrow = static_cast<const T*>(p.x) + row * p.ld;
-  Slice<T, G> sl(xrow, p.V, rank, G == 32 ? 0 : p.lg, t, mine);
-  uint64_t* bar = reinterpret_cast<uint64_t*>(&sc.bar);
-  if (t == 0) { mbar_init(bar, 1); mbar_fence_init(); }
-  if (ALT) {
-    if (t < kMaxAlt) sc.list[t] = 0;
-    if (G == 32) sc.list[t + 32] = 0;
-    if (t == 0) sc.count = 0;
-  }
-  group_sync<G>();
-  sl.fetch(bar);
-  float xid = 0.f;
+  if (G == 32 && row >= p.r.rows) return;
+  // shared memory: per warp a ring, whose place the scratch of the alternatives takes later, and its block maxima; what warps share and their lists of alternatives
+  const size_t per_warp = kRingBytes + (ALT ? (size_t)p.turns * 128 : 0);
+  uint4* ring = reinterpret_cast<uint4*>(reinterpret_cast<char*>(smem) + warp * per_warp);
+  WarpAlt& wa = *reinterpret_cast<WarpAlt*>(ring);
+  float* bm = reinterpret_cast<float*>(reinterpret_cast<char*>(ring) + kRingBytes);
+  Shared& sh = *reinterpret_cast<Shared*>(reinterpret_cast<char*>(smem) + W * per_warp);
+  RowAlt& ra = *reinterpret_cast<RowAlt*>(&sh + 1);
+  unsigned long long* lists = reinterpret_cast<unsigned long long*>(&ra + 1);   // [warps][n_alt]
+  const T* xrow = static_cast<const T*>(p.r.x) + row * p.r.ld;
+  const bool scribe = (G == 32 ? lane : threadIdx.x) == 0 && rank == 0;       // writes the row's numbers
   int id = -1;
-  if (t == 0 && rank == 0 && p.ids) {
-    id = dep_load(p.ids + row);
-    if (id >= 0 && id < p.V) xid = Elem<T>::load(xrow + id);
-  }
-  row_wait(bar, p.status);
-  typename Elem<T>::Max mx;
-  sl.each([&](const uint4& u) { mx.add(u); });
-  const float own = mx.value(), c = p.inv_tau * kLog2e;
-  float m, thr = 0.f;
-  if constexpr (ALT) m = part_max_and_threshold<T, G>(sl, sc, own, p.n_alt, thr);
-  else m = part_max<T, G, ALT>(sl, sc, own);
-  const Sums tot = part_sums<ENT>(sl, sc, safe_max(m), c);
-  if constexpr (ALT) {
-    part_candidates<T, G>(sl, sc, own, thr);
-    part_list<T, G>(sl, sc, p.n_alt);
-  }
-  const Part part{m, tot.s, tot.t};
-  Stat st;
-  unsigned long long* alts = sc.list;
-  if (G == 32 || parts == 1) {
-    st = stat_of<ENT>(m, tot.s, tot.t);
+  if (scribe && p.ids) id = dep_load(p.ids + row);
+  const Stream<T, G> st(xrow, p.r.V, rank, G == 32 ? 0 : p.r.lg, G == 32 ? lane : threadIdx.x);
+  const float c = p.r.inv_tau * kLog2e;
+  Online<T, ENT> on(c);
+  float partial_max = -INFINITY;
+  if (ALT)                             // the thread's last block, which may be short, and those that it does not have
+    for (int k = (st.t < st.nw ? (st.nw - st.t + G - 1) / G : 0) / Stream<T, G>::B; k < st.turns(); ++k) bm[k * 32 + lane] = -INFINITY;
+  st.each(ring, [&](const uint4* u, auto n, int k) {
+    const float b = on.template add<decltype(n)::value>(u);
+    if (ALT) {
+      if (k < 0) partial_max = b;
+      else if (decltype(n)::value > 1) bm[k * 32 + lane] = b;
+      else bm[k * 32 + lane] = fmaxf(bm[k * 32 + lane], b);
+    }
+  });
+  float xid = 0.f;
+  if (id >= 0 && id < p.r.V) xid = Elem<T>::load(xrow + id);
+  Part mine = on.part();
+  if constexpr (G == 32) {
+    const float m = warp_max(mine.m);
+    if (!is_near(safe_max(m), c)) mine = far_part<T, G, ENT>(st, ring, m, c);
+    const Part all = warp_union<ENT>(mine, c);
+    const Stat stat = stat_of<ENT>(all.m, all.s, all.t);
+    if constexpr (ALT) {
+      wa.gm[lane] = on.m;
+      __syncwarp();
+      const float thr = fmaxf(nth_of_32(wa.gm, p.n_alt, lane), Elem<T>::kLowest);   // -inf is no alternative
+      Found f;
+      warp_select(st, bm, partial_max, thr, p.n_alt, wa, f);
+      for (int i = lane; i < max(f.n, p.n_alt); i += 32) {    // every key's place is how many are larger
+        int place = i;
+        unsigned long long key = 0;
+        if (i < f.n) {
+          key = f.key[i];
+          place = 0;
+#pragma unroll 4
+          for (int j = 0; j < f.n; ++j) place += f.key[j] > key;
+        }
+        if (place < p.n_alt) tell_alt<ENT>(p, row, stat, place, key);
+      }
+    }
+    if (scribe) tell_row<T, ENT>(p, row, stat, id, xid);
   } else {
     __syncwarp();
-    cluster_wait();                      // every CTA of the cluster has started
-    if (t == 0) {
-      const uint32_t to = peer_smem(&sc.part[rank], 0);
-      peer_store(to, part.m); peer_store(to + 4, part.s); peer_store(to + 8, part.t);
-    }
-    if (ALT && t < p.n_alt) peer_store(peer_smem(&sc.peers[rank * kMaxAlt + t], 0), (uint64_t)sc.list[t]);
-    __syncwarp();
-    cluster_sync_all();
-    if (rank != 0) return;
-    st = stat_of_parts<ENT>(sc.part, parts, c, t & 31);
-    if constexpr (ALT) {                 // a key's place: its own, and how many of each other list are larger
-      alts = sc.cand;
-      if (t < p.n_alt) alts[t] = 0;
+    if (parts > 1) cluster_wait();     // every CTA of the cluster has started
+    if constexpr (ALT) {
+      // What every alternative reaches: the bound of this CTA's thread groups; in a cluster the largest of its CTAs' bounds, or that of
+      // groups over all of them.  The first holds where the large values lie in one part of the row, the second where they are spread.
+      const bool few = p.n_alt <= kFewAlt;
+      const int per = few ? 32 / W : kThreadGroups / W;        // groups of a warp
+      const float g = lane_group_max(on.m, per);
+      if (lane % (32 / per) == 0) ra.own[warp * per + lane / (32 / per)] = g;
       __syncthreads();
-      for (int i = t; i < parts * p.n_alt; i += G) {
-        const int l = i / p.n_alt;
-        int place = i - l * p.n_alt;
-        const unsigned long long key = sc.peers[l * kMaxAlt + place];
-        if (!key) continue;
-        for (int o = 0; o < parts && place < p.n_alt; ++o) {
-          if (o == l) continue;
-          int lo = 0, hi = p.n_alt;
-          while (lo < hi) {
-            const int mid = (lo + hi) >> 1;
-            if (sc.peers[o * kMaxAlt + mid] > key) lo = mid + 1; else hi = mid;
-          }
-          place += lo;
+      float thr = few ? nth_of_32(ra.own, p.n_alt, lane) : nth_of_128(ra.own, &ra.nth, p.n_alt);
+      if (parts > 1) {
+        const int gw = per >> p.r.lg;                          // groups of a warp where the cluster has 32 or 128 (at least one: 8 CTAs have 32 warps)
+        const float h = lane_group_max(on.m, gw);
+        const int i = lane >> p.r.lg;
+        const float v = __shfl_sync(0xFFFFFFFFu, h, i * (32 / gw) & 31);
+        if (i < gw) peer_store(peer_smem(&ra.all[(rank * W + warp) * gw + i], lane & (parts - 1)), v);
+        if ((int)threadIdx.x < parts) peer_store(peer_smem(&ra.bound[rank], threadIdx.x), thr);
+        __syncwarp();
+        cluster_sync_all();
+        for (int i = 0; i < parts; ++i) thr = fmaxf(thr, ra.bound[i]);
+        thr = fmaxf(thr, few ? nth_of_32(ra.all, p.n_alt, lane) : nth_of_128(ra.all, &ra.nth, p.n_alt));
+      }
+      thr = fmaxf(thr, Elem<T>::kLowest);                      // -inf is no alternative
+      Found f;
+      warp_select(st, bm, partial_max, thr, p.n_alt, wa, f);
+      if (f.n > p.n_alt) f.cut(p.n_alt);
+      unsigned long long* list = lists + (size_t)(rank * W + warp) * p.n_alt;
+      for (int i = lane; i < f.n; i += 32) peer_store(peer_smem(list + i, 0), (uint64_t)f.key[i]);
+      if (lane == 0) peer_store(peer_smem(&ra.count[rank * W + warp], 0), f.n);
+    }
+    share_parts<ENT>(sh, warp_union<ENT>(mine, c), 0, parts, rank, warp, lane);
+    const int warps = parts * W;
+    const float m = warp_max(lane < warps ? sh.part[0][lane].m : -INFINITY);
+    const bool near = is_near(safe_max(m), c);
+    if (!near) share_parts<ENT>(sh, warp_union<ENT>(far_part<T, G, ENT>(st, ring, m, c), c), 1, parts, rank, warp, lane);
+    if (rank != 0 || (!ALT && warp != 0)) return;
+    const Stat stat = stat_of_parts<ENT>(sh.part[near ? 0 : 1], warps, c, lane);
+    if constexpr (ALT) {               // every key's place is how many are larger
+      const int per = kStreamThreads / warps, l = threadIdx.x / per;   // threads of a list; this thread's
+      int total = 0;
+      for (int i = 0; i < warps; ++i) total += ra.count[i];
+      for (int i = threadIdx.x % per; i < ra.count[l]; i += per) {
+        const unsigned long long key = lists[(size_t)l * p.n_alt + i];
+        int place = 0;
+        for (int o = 0; o < warps; ++o) {
+          const unsigned long long* k = lists + (size_t)o * p.n_alt;
+          const int n = ra.count[o];
+#pragma unroll 4
+          for (int j = 0; j < n; ++j) place += k[j] > key;
         }
-        if (place < p.n_alt) alts[place] = key;
+        if (place < p.n_alt) tell_alt<ENT>(p, row, stat, place, key);
       }
-      __syncthreads();
+      if ((int)threadIdx.x >= total && (int)threadIdx.x < p.n_alt) tell_alt<ENT>(p, row, stat, threadIdx.x, 0ull);
     }
-  }
-  if (ALT)
-    for (int i = t; i < p.n_alt; i += G) {
-      const unsigned long long key = alts[i];
-      const bool bad = st.L != st.L;
-      const float lp = bad ? st.L : key ? (alt_value(key) - st.m) * p.inv_tau - st.L : -INFINITY;
-      p.alt_ids[(size_t)row * p.n_alt + i] = bad || !key ? -1 : alt_index(key);
-      p.alt_logprob[(size_t)row * p.n_alt + i] = lp;
-    }
-  if (t == 0) {
-    if (p.stats) p.stats[row] = make_float2(st.m, st.L);
-    if (ENT) p.entropy[row] = st.H;
-    if (p.logprob) {
-      float lp = 0.f;                    // -1: the row has no token
-      if (id >= 0 && id < p.V) {
-        lp = st.L == -INFINITY ? -INFINITY : (xid - st.m) * p.inv_tau - st.L;
-      } else if (id != -1) {
-        put_status(p.status, DEV_BAD_TOKEN_ID);
-        lp = __int_as_float(0x7FC00000);
-      }
-      p.logprob[row] = lp;
-    }
+    if (scribe) tell_row<T, ENT>(p, row, stat, id, xid);
   }
 }
 
 // ---- distillation: loss, and with GRAD its gradient while the row is still in shared memory --------------------------------
 struct DistillArgs {
-  const void* x; long long ld; int rows, V, per_max, lg;
-  float inv_tau;
+  RowsArgs r;
   const int32_t* t_ids; const float* t_logits; int K;
   const float* g;                  // [rows] or null: 1
   float* loss; float2* stats;
   void* dx; long long ld_dx;
-  int32_t* status;
 };
 
-// The teacher's row: lane l of one warp holds the entries l, l + 32, ...; q over the entries that have a token (-1: none).
-struct Teacher {
+// The teacher's row: lane l of one warp holds the entries l, l + 32, ...; q over the entries that have a token (-1: none), lq = ln q.
+struct TeacherEntries {
   static constexpr int P = kMaxTeacher / 32;
+  int id[P];
+  float x[P];
+  __device__ __forceinline__ void load(const int32_t* ids, const float* logits, int K, int lane) {
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+      id[i] = -1;
+      x[i] = -INFINITY;
+      if (lane + 32 * i < K) { id[i] = dep_load(ids + lane + 32 * i); x[i] = dep_load(logits + lane + 32 * i); }
+    }
+  }
+};
+struct Teacher {
+  static constexpr int P = TeacherEntries::P;
   int id[P];
   float q[P], lq[P];
   bool some, bad;
-  __device__ __forceinline__ void load(const int32_t* ids, const float* logits, int K, int V, float inv_tau, int lane) {
+  __device__ __forceinline__ void weigh(const TeacherEntries& e, int K, int V, float inv_tau) {
     float x[P], m = -INFINITY;
     bool wrong = false, any = false;
 #pragma unroll
     for (int i = 0; i < P; ++i) {
-      const int k = lane + 32 * i;
-      id[i] = -1;
-      x[i] = -INFINITY;
-      if (32 * i >= K) continue;
-      if (k < K) {
-        const int v = dep_load(ids + k);
-        if (v >= 0 && v < V) {
-          id[i] = v;
-          x[i] = dep_load(logits + k);
-        } else {
-          wrong |= v != -1;
-        }
-      }
+      const bool has = e.id[i] >= 0 && e.id[i] < V;
+      wrong |= !has && e.id[i] != -1;
+      id[i] = has ? e.id[i] : -1;
+      x[i] = has ? e.x[i] : -INFINITY;
       any |= x[i] != -INFINITY;
       m = fmaxf(m, x[i]);
     }
@@ -655,34 +839,72 @@ struct Teacher {
     s = warp_sum(s);
     some = __any_sync(0xFFFFFFFFu, any);
     bad = __any_sync(0xFFFFFFFFu, wrong);
-    const float ls = logf(s);
+    const float ls = logf(s), inv = 1.f / s;
 #pragma unroll
     for (int i = 0; i < P; ++i) {
       if (32 * i >= K) continue;
-      q[i] = some ? q[i] / s : 0.f;
+      q[i] = some ? q[i] * inv : 0.f;
       lq[i] -= ls;
     }
   }
 };
-struct alignas(16) TeacherRow {    // of one row, for the gradient's corrections
+struct alignas(16) TeacherRow {    // the same in shared memory; behind K: id -1
   int id[kMaxTeacher];
-  float q[kMaxTeacher], x[kMaxTeacher];
-  int some;
-};
-// What entry k, which has a token, takes off its probability: all entries of that token together, at the first of them; -1 elsewhere.
-__device__ __forceinline__ float teacher_share(const TeacherRow& tr, int k, int K) {
-  const int id = tr.id[k];
-  float sum = 0.f;
-  bool first = true;
-  for (int j = 0; j < K; j += 4) {         // (behind K: id -1)
-    const int4 o = *reinterpret_cast<const int4*>(tr.id + j);
-    const float4 q = *reinterpret_cast<const float4*>(tr.q + j);
-    if (o.x == id) { sum += q.x; first &= j >= k; }
-    if (o.y == id) { sum += q.y; first &= j + 1 >= k; }
-    if (o.z == id) { sum += q.z; first &= j + 2 >= k; }
-    if (o.w == id) { sum += q.w; first &= j + 3 >= k; }
+  float q[kMaxTeacher];
+  int some;                       // whether it has an entry
+  __device__ __forceinline__ void put(const Teacher& te, int lane) {
+#pragma unroll
+    for (int i = 0; i < Teacher::P; ++i) { id[lane + 32 * i] = te.id[i]; q[lane + 32 * i] = te.q[i]; }
   }
-  return first ? sum : -1.f;
+};
+// What an entry takes off its token's probability: q, where no token comes twice; else all entries of the token together, at the first of them, -1 at the
+// others.  tr holds what te does.
+__device__ __forceinline__ void teacher_shares(const Teacher& te, const TeacherRow& tr, int K, int lane, float (&share)[Teacher::P]) {
+  constexpr int P = Teacher::P;
+  bool twice = false;
+#pragma unroll
+  for (int i = 0; i < P; ++i) {
+    share[i] = te.id[i] >= 0 ? te.q[i] : -1.f;
+    if (32 * i >= K) continue;
+    const uint32_t same = __match_any_sync(0xFFFFFFFFu, te.id[i]);
+    twice |= te.id[i] >= 0 && (same & (same - 1)) != 0;
+#pragma unroll
+    for (int j = 0; j < i; ++j)
+#pragma unroll 8
+      for (int r = 0; r < 32; ++r) {
+        const int other = __shfl_sync(0xFFFFFFFFu, te.id[j], (lane + r) & 31);   // (by every lane)
+        twice |= te.id[i] >= 0 && te.id[i] == other;
+      }
+  }
+  if (!__any_sync(0xFFFFFFFFu, twice)) return;
+  for (int i = 0; i < P; ++i) {
+    const int k = lane + 32 * i, id = tr.id[k];
+    float sum = 0.f;
+    bool first = id >= 0;
+    for (int j = 0; j < K; ++j) {
+      if (tr.id[j] != id) continue;
+      sum += tr.q[j];
+      first &= j >= k;
+    }
+    const float s = first ? sum : -1.f;
+#pragma unroll
+    for (int n = 0; n < P; ++n) share[n] = n == i ? s : share[n];
+  }
+}
+
+// The row's loss and statistics, by the warp that has the teacher's entries; x: the logits of their tokens.
+__device__ __forceinline__ void tell_loss(const DistillArgs& p, int row, const Teacher& te, const float (&x)[Teacher::P], const Stat& st, int lane) {
+  float loss = 0.f;
+#pragma unroll
+  for (int i = 0; i < Teacher::P; ++i) {
+    const float lp = st.L == -INFINITY ? -INFINITY : (x[i] - st.m) * p.r.inv_tau - st.L;
+    if (te.id[i] >= 0 && te.q[i] != 0.f) loss = fmaf(te.q[i], te.lq[i] - lp, loss);   // (q NaN: the loss too)
+  }
+  loss = warp_sum(loss);
+  if (lane != 0) return;
+  if (te.bad) { put_status(p.r.status, DEV_BAD_TOKEN_ID); loss = __int_as_float(0x7FC00000); }
+  p.loss[row] = loss;
+  if (p.stats) p.stats[row] = make_float2(st.m, st.L);
 }
 
 template <typename T> __device__ __forceinline__ bool same_alignment(const T* a, const T* b) {
@@ -714,97 +936,144 @@ template <typename T, int G, typename F> __device__ __forceinline__ void write_r
   }
 }
 
-template <int G> struct alignas(16) DistillScratch { Scratch<G, false> sc; TeacherRow tr; };
-
-template <typename T, int G, bool GRAD>
-__global__ void __launch_bounds__(cta_threads<G>()) distill_kernel(const DistillArgs p) {
-  using S = DistillScratch<G>;
-  extern __shared__ uint4 smem[];
-  pdl_trigger();
-  const int parts = G == 32 ? 1 : 1 << p.lg, rank = G == 32 ? 0 : (int)cluster_ctarank();
-  const int sub = G == 32 ? threadIdx.x >> 5 : 0, t = G == 32 ? threadIdx.x & 31 : threadIdx.x;
-  const int row = G == 32 ? blockIdx.x * kWarpRows + sub : blockIdx.x >> p.lg;
-  pdl_wait();
-  if (G == 32 && row >= p.rows) return;
-  if (G > 32 && parts > 1) cluster_arrive_relaxed();
-  uint4* mine = reinterpret_cast<uint4*>(reinterpret_cast<char*>(smem) + sub * group_bytes<S>(p.per_max));
-  S& own = *reinterpret_cast<S*>(mine + p.per_max);
-  Scratch<G, false>& sc = own.sc;
-  TeacherRow& tr = own.tr;
-  const T* xrow = static_cast<const T*>(p.x) + row * p.ld;
-  Slice<T, G> sl(xrow, p.V, rank, G == 32 ? 0 : p.lg, t, mine);
-  uint64_t* bar = reinterpret_cast<uint64_t*>(&sc.bar);
-  if (t == 0) { mbar_init(bar, 1); mbar_fence_init(); }
-  group_sync<G>();
-  sl.fetch(bar);
-  Teacher te;
-  float xk[Teacher::P];
-  if (t < 32 && (GRAD || rank == 0)) {
-    te.load(p.t_ids + (size_t)row * p.K, p.t_logits + (size_t)row * p.K, p.K, p.V, p.inv_tau, t);
-#pragma unroll
-    for (int i = 0; i < Teacher::P; ++i) {
-      xk[i] = 0.f;
-      if (GRAD || 32 * i < p.K) xk[i] = te.id[i] >= 0 ? Elem<T>::load(xrow + te.id[i]) : 0.f;
-      if (GRAD) { tr.id[t + 32 * i] = te.id[i]; tr.q[t + 32 * i] = te.q[i]; tr.x[t + 32 * i] = xk[i]; }
-    }
-    if (GRAD && t == 0) tr.some = te.some;
-  }
-  row_wait(bar, p.status);
+// G threads go over the row; one more warp deals with the teacher meanwhile: it weighs the entries, reads their tokens' logits, adds up the entries of
+// the same token, and at the end writes the loss and puts the gradient of those tokens right.
+// What every thread finds in its vectors: their maximum, and the sums against it.  No barrier: the warps' results are put together once.
+template <typename T, int G> __device__ __forceinline__ Part thread_part(const Slice<T, G>& sl, float c) {
   typename Elem<T>::Max mx;
   sl.each([&](const uint4& u) { mx.add(u); });
-  const float m = part_max<T, G, false>(sl, sc, mx.value()), c = p.inv_tau * kLog2e;
-  const Sums tot = part_sums<false>(sl, sc, safe_max(m), c);
-  const Part part{m, tot.s, 0.f};
-  Stat st;
-  if (G == 32 || parts == 1) {
-    st = stat_of<false>(m, tot.s, 0.f);
+  const float m = mx.value(), m0 = safe_max(m);
+  Sums<T, false> sums;
+  if (__all_sync(0xFFFFFFFFu, is_near(m0, c))) {
+    const float R = whole_ref(m0, c);
+    sl.each([&, ex = Expo<true>(R, c)](const uint4& u) { sums.add(u, ex); });
+    return part_of(m, sums, delta(m0, c, R));
+  }
+  sl.each([&, ex = Expo<false>(m0, c)](const uint4& u) { sums.add(u, ex); });
+  return part_of(m, sums, 0.f);
+}
+
+struct alignas(16) DistillScratch { Part part[64]; TeacherRow tr; };
+
+template <typename T, int G>
+__global__ void __launch_bounds__(G + 32, G == 64 ? 10 : 768 / G) distill_kernel(const DistillArgs p) {
+  constexpr int W = G / 32, E = Elem<T>::E, P = Teacher::P;
+  extern __shared__ uint4 smem[];
+  pdl_trigger();
+  const int parts = 1 << p.r.lg, rank = parts > 1 ? (int)cluster_ctarank() : 0, t = threadIdx.x, warp = t >> 5, lane = t & 31, row = blockIdx.x >> p.r.lg;
+  DistillScratch& sc = *reinterpret_cast<DistillScratch*>(smem + p.r.per_max);
+  TeacherRow& tr = sc.tr;
+  if (parts > 1) cluster_arrive_relaxed();
+  pdl_wait();
+  const float c = p.r.inv_tau * kLog2e;
+  const T* xrow = static_cast<const T*>(p.r.x) + row * p.r.ld;
+  T* drow = static_cast<T*>(p.dx) + row * p.ld_dx;
+  const Slice<T, G> sl(xrow, p.r.V, rank, p.r.lg, t, smem);
+  const float wg = (p.g ? dep_load(p.g + row) : 1.f) * p.r.inv_tau;
+  // Two barriers: behind the first the parts are complete, the logits of the teacher's tokens read (in place they are overwritten next) and tr.some is
+  // written; behind the second the row's gradient is written.
+  if (warp < W) {
+    sl.fetch();
+    cp_async_wait_all();
+    const Part part = warp_union<false>(thread_part(sl, c), c);
+    __syncwarp();
+    if (parts == 1) {
+      if (lane == 0) sc.part[warp] = part;
+      __syncthreads();
+    } else {
+      cluster_wait();                  // every CTA of the cluster has started
+      if (lane < parts) {
+        const uint32_t to = peer_smem(&sc.part[rank * W + warp], lane);
+        peer_store(to, part.m); peer_store(to + 4, part.s); peer_store(to + 8, 0.f);
+      }
+      __syncwarp();
+      cluster_sync_all();
+    }
+    const Stat st = stat_of_parts<false>(sc.part, parts * W, c, lane);
+    if (!tr.some || wg == 0.f || st.L == -INFINITY) {
+      write_row<T, G>(sl, drow, [](uint64_t) { return uint64_t(0); });
+    } else if (is_near(st.m, c)) {
+      const float R = whole_ref(st.m, c), f = wg / st.s * exp2_fast(delta(st.m, c, R));
+      write_row<T, G>(sl, drow, [ex = Expo<true>(R, c), f2 = pack2(f, f)](uint64_t x) { return mul2(exp2_pair(ex(x)), f2); });
+    } else {
+      const float f = wg / st.s;
+      write_row<T, G>(sl, drow, [ex = Expo<false>(st.m, c), f2 = pack2(f, f)](uint64_t x) { return mul2(exp2_pair(ex(x)), f2); });
+    }
+    __syncthreads();
+    return;
+  }
+  Teacher te;
+  float x[P], share[P], keep = 0.f;
+  TeacherEntries entries;
+  entries.load(p.t_ids + (size_t)row * p.K, p.t_logits + (size_t)row * p.K, p.K, lane);
+#pragma unroll
+  for (int i = 0; i < P; ++i) x[i] = entries.id[i] >= 0 && entries.id[i] < p.r.V ? Elem<T>::load(xrow + entries.id[i]) : 0.f;
+  te.weigh(entries, p.K, p.r.V, p.r.inv_tau);
+  if (lane == 0) tr.some = te.some;
+  tr.put(te, lane);
+  __syncwarp();
+  teacher_shares(te, tr, p.K, lane, share);
+#pragma unroll
+  for (int i = 0; i < P; ++i) keep += x[i];
+  asm volatile("" ::"f"(keep) : "memory");   // the logits have arrived
+  __syncwarp();
+  if (parts > 1) { cluster_wait(); cluster_sync_all(); }
+  else __syncthreads();
+  const Stat st = stat_of_parts<false>(sc.part, parts * W, c, lane);
+  if (rank == 0) tell_loss(p, row, te, x, st, lane);
+  __syncthreads();
+  if (te.some && wg != 0.f && st.L != -INFINITY) {
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+      const int id = te.id[i], at = id < 0 ? -1 : (id + sl.off) / E - sl.v0;
+      if (at >= 0 && at < sl.n && !(share[i] < 0.f)) Elem<T>::store(drow + id, wg * (exp2_fast((x[i] - st.m) * c) / st.s - share[i]));
+    }
+  }
+}
+
+// The loss alone: nothing of the row is needed again but the logits of the teacher's tokens.
+template <typename T, int G>
+__global__ void __launch_bounds__(kStreamThreads, 8) distill_loss_kernel(const DistillArgs p) {
+  constexpr int W = kStreamWarps;
+  __shared__ Shared sh;
+  __shared__ uint4 rings[W][kRingBytes / 16];
+  pdl_trigger();
+  const int parts = G == 32 ? 1 : 1 << p.r.lg, rank = parts > 1 ? (int)cluster_ctarank() : 0, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int row = G == 32 ? blockIdx.x * W + warp : blockIdx.x >> p.r.lg;
+  if (parts > 1) cluster_arrive_relaxed();
+  pdl_wait();
+  if (G == 32 && row >= p.r.rows) return;
+  const T* xrow = static_cast<const T*>(p.r.x) + row * p.r.ld;
+  const Stream<T, G> st(xrow, p.r.V, rank, G == 32 ? 0 : p.r.lg, G == 32 ? lane : threadIdx.x);
+  uint4* ring = rings[warp];
+  const float c = p.r.inv_tau * kLog2e;
+  Online<T, false> on(c);
+  st.each(ring, [&](const uint4* u, auto n, int) { on.template add<decltype(n)::value>(u); });
+  Part mine = on.part();
+  Stat stat;
+  if constexpr (G == 32) {
+    const float m = warp_max(mine.m);
+    if (!is_near(safe_max(m), c)) mine = far_part<T, G, false>(st, ring, m, c);
+    const Part all = warp_union<false>(mine, c);
+    stat = stat_of<false>(all.m, all.s, all.t);
   } else {
     __syncwarp();
-    cluster_wait();
-    if (t < (GRAD ? parts : 1)) {
-      const uint32_t to = peer_smem(&sc.part[rank], t);
-      peer_store(to, part.m); peer_store(to + 4, part.s); peer_store(to + 8, 0.f);
-    }
-    __syncwarp();
-    cluster_sync_all();                  // in place: and every CTA has read the logits of the teacher's tokens
-    if (!GRAD && rank != 0) return;
-    st = stat_of_parts<false>(sc.part, parts, c, t & 31);
+    if (parts > 1) cluster_wait();     // every CTA of the cluster has started
+    share_parts<false>(sh, warp_union<false>(mine, c), 0, parts, rank, warp, lane);
+    const float m = warp_max(lane < parts * W ? sh.part[0][lane].m : -INFINITY);
+    const bool near = is_near(safe_max(m), c);
+    if (!near) share_parts<false>(sh, warp_union<false>(far_part<T, G, false>(st, ring, m, c), c), 1, parts, rank, warp, lane);
+    if (rank != 0 || warp != 0) return;
+    stat = stat_of_parts<false>(sh.part[near ? 0 : 1], parts * W, c, lane);
   }
-  if (rank == 0 && t < 32) {
-    float loss = 0.f;
+  TeacherEntries entries;
+  entries.load(p.t_ids + (size_t)row * p.K, p.t_logits + (size_t)row * p.K, p.K, lane);
+  float x[Teacher::P];
 #pragma unroll
-    for (int i = 0; i < Teacher::P; ++i) {
-      const float lp = st.L == -INFINITY ? -INFINITY : (xk[i] - st.m) * p.inv_tau - st.L;
-      if (te.id[i] >= 0 && te.q[i] != 0.f) loss = fmaf(te.q[i], te.lq[i] - lp, loss);   // (q NaN: the loss too)
-    }
-    loss = warp_sum(loss);
-    if (t == 0) {
-      if (te.bad) { put_status(p.status, DEV_BAD_TOKEN_ID); loss = __int_as_float(0x7FC00000); }
-      p.loss[row] = loss;
-      if (p.stats) p.stats[row] = make_float2(st.m, st.L);
-    }
-  }
-  if constexpr (GRAD) {
-    constexpr int E = Elem<T>::E;
-    T* drow = static_cast<T*>(p.dx) + row * p.ld_dx;
-    const float w = (p.g ? dep_load(p.g + row) : 1.f) * p.inv_tau;
-    const bool none = !tr.some || w == 0.f || st.L == -INFINITY;   // (tr: written before the barriers of the sums)
-    const bool near = is_near(st.m, c);
-    const float f = none ? 0.f : near ? w / st.s * fmaf(-kLn2, Expo<true>::slip(st.m, c), 1.f) : w / st.s;
-    if (none) write_row<T, G>(sl, drow, [&](uint64_t) { return uint64_t(0); });
-    else if (near) write_row<T, G>(sl, drow, [&, ex = Expo<true>(st.m, c), f2 = pack2(f, f)](uint64_t x) { return mul2(exp2_pair(ex(x)), f2); });
-    else write_row<T, G>(sl, drow, [&, ex = Expo<false>(st.m, c), f2 = pack2(f, f)](uint64_t x) { return mul2(exp2_pair(ex(x)), f2); });
-    group_sync<G>();
-    if (!none)
-      for (int k = t; k < p.K; k += G) {
-        const int id = tr.id[k];
-        const int at = id < 0 ? -1 : (id + sl.off) / E - sl.v0;
-        if (at < 0 || at >= sl.n) continue;
-        const float share = teacher_share(tr, k, p.K);
-        if (share < 0.f) continue;
-        Elem<T>::store(drow + id, w * (exp2_fast((tr.x[k] - st.m) * c) / st.s - share));
-      }
-  }
+  for (int i = 0; i < Teacher::P; ++i) x[i] = entries.id[i] >= 0 && entries.id[i] < p.r.V ? Elem<T>::load(xrow + entries.id[i]) : 0.f;
+  Teacher te;
+  te.weigh(entries, p.K, p.r.V, p.r.inv_tau);
+  tell_loss(p, row, te, x, stat, lane);
 }
 
 // ---- gradients for weights that come after the forward call ---------------------------------------------------------------
@@ -946,8 +1215,10 @@ __global__ void __launch_bounds__(32 * kGradWarps) distill_grad_kernel(const Gra
   const Segment<T, U> sg(xrow, drow, p.V, seg, lane);
   uint4 x[U];
   sg.load(x);
+  TeacherEntries entries;
+  entries.load(p.t_ids + (size_t)row * p.K, p.t_logits + (size_t)row * p.K, p.K, lane);
   Teacher te;
-  te.load(p.t_ids + (size_t)row * p.K, p.t_logits + (size_t)row * p.K, p.K, p.V, p.inv_tau, lane);
+  te.weigh(entries, p.K, p.V, p.inv_tau);
   if (te.bad && seg == 0 && lane == 0) put_status(p.status, DEV_BAD_TOKEN_ID);
   const float m = dep_load(&p.stats[row].x), L = dep_load(&p.stats[row].y);
   const float w = (p.g_logprob ? dep_load(p.g_logprob + row) : 1.f) * p.inv_tau;
@@ -955,15 +1226,18 @@ __global__ void __launch_bounds__(32 * kGradWarps) distill_grad_kernel(const Gra
     sg.zero();
     return;
   }
+  float xk[Teacher::P];
+  tr.put(te, lane);
   const int from = seg * 32 * U * E - sg.off, lo = max(0, from), hi = min(p.V, from + 32 * U * E);   // the logits of this warp
 #pragma unroll
   for (int i = 0; i < Teacher::P; ++i) {
     const int id = te.id[i];
-    tr.id[lane + 32 * i] = id;
-    tr.q[lane + 32 * i] = te.q[i];
-    if (id >= lo && id < hi) tr.x[lane + 32 * i] = Elem<T>::load(xrow + id);
+    xk[i] = 0.f;
+    if (id >= lo && id < hi) xk[i] = Elem<T>::load(xrow + id);
   }
-  __syncwarp();
+  __syncwarp();                        // in place: read before any lane writes
+  float share[Teacher::P];
+  teacher_shares(te, tr, p.K, lane, share);
   const float c = p.inv_tau * kLog2e, L2 = L * kLog2e;
   const LogP logp(m, c, L2);
 #pragma unroll
@@ -980,11 +1254,10 @@ __global__ void __launch_bounds__(32 * kGradWarps) distill_grad_kernel(const Gra
     sg.store(u, d);
   }
   __syncwarp();
-  for (int k = lane; k < p.K; k += 32) {
-    const int id = tr.id[k];
-    if (id < lo || id >= hi) continue;
-    const float share = teacher_share(tr, k, p.K);
-    if (share >= 0.f || share != share) Elem<T>::store(drow + id, w * (exp2_fast(fmaf(tr.x[k] - m, c, -L2)) - share));
+#pragma unroll
+  for (int i = 0; i < Teacher::P; ++i) {
+    const int id = te.id[i];
+    if (id >= lo && id < hi && !(share[i] < 0.f)) Elem<T>::store(drow + id, w * (exp2_fast(fmaf(xk[i] - m, c, -L2)) - share[i]));
   }
 }
 
@@ -1004,21 +1277,34 @@ cudaError_t launch_clusters(void (*kernel)(KArgs...), unsigned grid, int threads
   return cudaLaunchKernelEx(&cfg, kernel, static_cast<KArgs>(args)...);
 }
 
-// Who takes a row: a warp, or a cluster of CTAs of 128 or 256 threads.
-struct Shape { int group, lg, per_max; };
+// Who takes a row.  Streamed: a warp, or a cluster of CTAs of 128 threads.  Kept in shared memory: a cluster of CTAs of 64, 128 or 256 threads.
+struct Shape { int group, lg, per_max; };   // per_max: vectors of the largest part
 constexpr int kMaxRowBytes = 1536 << 10;
-static int envi(const char* n, int d) { const char* s = getenv(n); return s ? atoi(s) : d; }
-Shape row_shape(const void* x, long long ld, int rows, int V, int es, bool warp_may) {
-  const int E = 16 / es;
+int row_vectors(const void* x, long long ld, int V, int es) {
   const bool aligned = (reinterpret_cast<uintptr_t>(x) & 15u) == 0 && (ld * es) % 16 == 0;   // every row starts on a boundary
-  const int nv = aligned ? (V + E - 1) / E : logits_vectors(V, E);
-  static const int WV = envi("FV_WV", 1024), G1 = envi("FV_G1", 128), N1 = envi("FV_N1", 2048), SL = envi("FV_SL", 48), WR = envi("FV_WR", 8), LM = envi("FV_LM", 512);
-  if (warp_may && nv <= WV && rows >= 148 * WR) return {32, 0, nv};
+  return aligned ? (V + 16 / es - 1) / (16 / es) : logits_vectors(V, 16 / es);
+}
+// CTAs that share a row, as a logarithm: as many as give every SM one, while a part has at least 1024 vectors (16 KB; below that the cluster's barriers cost what
+// the shorter part saves: one row of 32 KB 2.5 us on one CTA, 2.3 on two; of 256 KB 8.2 on one, 2.8 on eight).
+int spread(int nv, int rows, int lg) {
+  while ((1 << lg) < kMaxCluster && ((long long)rows << lg) < 148 && (nv >> (lg + 1)) >= 1024) ++lg;
+  return lg;
+}
+// A warp to a row where rows are short or so many that the warps fill the GPU: no barrier, a quarter of the instructions that a row takes beside its logits.
+// us, a warp / a CTA of four, fp32, entropy alone and with 8 alternatives: 600 rows of 4 KB 2.2 / 3.0, 4.0 / 7.8; 1200 of 16 KB 5.7 / 4.7, 9.2 / 10.5; 4800 of 16 KB 9.3 / 13.1, 13.4 / 30.2;
+// 4800 of 32 KB 27 / 26, 32 / 40; 2400 of 64 KB 32 / 27, 33 / 35; 2400 of 128 KB 58 / 51, 70 / 58.  More alternatives than a warp's 32 lanes can bound take the CTA.
+Shape stream_shape(int nv, int rows, int n_alt) {
+  if (n_alt <= kFewAlt && (nv <= 512 || (nv <= 1024 && rows >= 148 * 8) || (nv <= 2048 && rows >= 148 * 24))) return {32, 0, nv};
+  const int lg = spread(nv, rows, 0);
+  return {128, lg, (nv + (1 << lg) - 1) >> lg};
+}
+// Parts of at most 32 KB, six to an SM: us for 4096 rows of 256 KB, 64 threads to a part of up to 2048 vectors 455, 128 383, 256 568; parts of 64 KB and 256 threads 386.
+Shape kept_shape(int nv, int rows) {
   int lg = 0;
-  while ((1 << lg) < kMaxCluster && (size_t)((nv + (1 << lg) - 1) >> lg) * 16 > ((size_t)SL << 10)) ++lg;
-  while ((1 << lg) < kMaxCluster && ((long long)rows << lg) < 148 && (nv >> (lg + 1)) >= LM) ++lg;
+  while ((1 << lg) < kMaxCluster && (nv + (1 << lg) - 1) >> lg > 2048) ++lg;
+  lg = spread(nv, rows, lg);
   const int per = (nv + (1 << lg) - 1) >> lg;
-  return {per <= N1 ? G1 : 256, lg, per};
+  return {per <= 1024 ? 64 : per <= 2048 ? 128 : 256, lg, per};
 }
 
 constexpr int kMaxSmem = 227 << 10;
@@ -1028,11 +1314,10 @@ template <typename T> cudaError_t allow_all() {
   auto add = [&](auto kernel) { if (e == cudaSuccess) e = allow_smem(kernel); };
   auto group = [&](auto g) {
     constexpr int G = decltype(g)::value;
-    add(token_logprobs_kernel<T, G, false, false>); add(token_logprobs_kernel<T, G, false, true>);
-    add(token_logprobs_kernel<T, G, true, false>); add(token_logprobs_kernel<T, G, true, true>);
-    add(distill_kernel<T, G, false>); add(distill_kernel<T, G, true>);
+    add(token_logprobs_kernel<T, G, false, true>); add(token_logprobs_kernel<T, G, true, true>);
   };
-  group(std::integral_constant<int, 32>()); group(std::integral_constant<int, 128>()); group(std::integral_constant<int, 256>());
+  group(std::integral_constant<int, 32>()); group(std::integral_constant<int, 128>());
+  add(distill_kernel<T, 64>); add(distill_kernel<T, 128>); add(distill_kernel<T, 256>);
   return e;
 }
 // Function attributes belong to a device: set on the first call on each.
@@ -1047,32 +1332,33 @@ cudaError_t logits_init() {
   return e;
 }
 
-template <typename F> cudaError_t with_group(int group, F f) {
-  if (group == 32) return f(std::integral_constant<int, 32>());
-  return group == 128 ? f(std::integral_constant<int, 128>()) : f(std::integral_constant<int, 256>());
+template <typename K, typename A> cudaError_t go_rows(K kernel, int threads, A& a, const Shape& s, size_t smem, cudaStream_t st) {
+  a.r.per_max = s.per_max; a.r.lg = s.lg;
+  const unsigned grid = s.group == 32 ? (a.r.rows + kStreamWarps - 1) / kStreamWarps : (unsigned)a.r.rows << s.lg;
+  return launch_clusters(kernel, grid, threads, 1 << s.lg, smem, st, a);
 }
-template <int G, typename K, typename A> cudaError_t go_rows(K kernel, const A& a, size_t bytes, cudaStream_t st) {   // bytes: of a group's shared memory
-  const unsigned grid = G == 32 ? (a.rows + kWarpRows - 1) / kWarpRows : (unsigned)a.rows << a.lg;
-  return launch_clusters(kernel, grid, cta_threads<G>(), 1 << a.lg, bytes * (G == 32 ? kWarpRows : 1), st, a);
+template <typename T, int G> cudaError_t go_token(TokenArgs& a, const Shape& s, cudaStream_t st) {
+  a.turns = (s.per_max + Stream<T, G>::B * G - 1) / (Stream<T, G>::B * G);
+  const size_t rows = kStreamWarps * (size_t)kRingBytes + (G == 32 ? 0 : sizeof(Shared));
+  const size_t with = rows + kStreamWarps * (size_t)a.turns * 128 + (G == 32 ? 0 : sizeof(RowAlt) + ((size_t)a.n_alt * kStreamWarps * 8 << s.lg));
+  if (a.n_alt > 0)
+    return a.entropy ? go_rows(token_logprobs_kernel<T, G, true, true>, kStreamThreads, a, s, with, st) : go_rows(token_logprobs_kernel<T, G, false, true>, kStreamThreads, a, s, with, st);
+  return a.entropy ? go_rows(token_logprobs_kernel<T, G, true, false>, kStreamThreads, a, s, rows, st) : go_rows(token_logprobs_kernel<T, G, false, false>, kStreamThreads, a, s, rows, st);
 }
-template <typename T> cudaError_t launch_token(RowsArgs& a, cudaStream_t st) {
-  const Shape s = row_shape(a.x, a.ld, a.rows, a.V, sizeof(T), a.n_alt <= kFewAlt);
-  a.per_max = s.per_max; a.lg = s.lg;
-  return with_group(s.group, [&](auto g) {
-    constexpr int G = decltype(g)::value;
-    const size_t with = group_bytes<Scratch<G, true>>(s.per_max), without = group_bytes<Scratch<G, false>>(s.per_max);
-    if (a.n_alt > 0) return a.entropy ? go_rows<G>(token_logprobs_kernel<T, G, true, true>, a, with, st) : go_rows<G>(token_logprobs_kernel<T, G, false, true>, a, with, st);
-    return a.entropy ? go_rows<G>(token_logprobs_kernel<T, G, true, false>, a, without, st) : go_rows<G>(token_logprobs_kernel<T, G, false, false>, a, without, st);
-  });
+template <typename T> cudaError_t launch_token(TokenArgs& a, cudaStream_t st) {
+  const Shape s = stream_shape(row_vectors(a.r.x, a.r.ld, a.r.V, sizeof(T)), a.r.rows, a.n_alt);
+  return s.group == 32 ? go_token<T, 32>(a, s, st) : go_token<T, 128>(a, s, st);
 }
 template <typename T> cudaError_t launch_distill(DistillArgs& a, cudaStream_t st) {
-  const Shape s = row_shape(a.x, a.ld, a.rows, a.V, sizeof(T), true);
-  a.per_max = s.per_max; a.lg = s.lg;
-  return with_group(s.group, [&](auto g) {
-    constexpr int G = decltype(g)::value;
-    const size_t bytes = group_bytes<DistillScratch<G>>(s.per_max);
-    return a.dx ? go_rows<G>(distill_kernel<T, G, true>, a, bytes, st) : go_rows<G>(distill_kernel<T, G, false>, a, bytes, st);
-  });
+  const int nv = row_vectors(a.r.x, a.r.ld, a.r.V, sizeof(T));
+  if (!a.dx) {
+    const Shape s = stream_shape(nv, a.r.rows, 0);
+    return s.group == 32 ? go_rows(distill_loss_kernel<T, 32>, kStreamThreads, a, s, 0, st) : go_rows(distill_loss_kernel<T, 128>, kStreamThreads, a, s, 0, st);
+  }
+  const Shape s = kept_shape(nv, a.r.rows);
+  const size_t smem = (size_t)s.per_max * 16 + sizeof(DistillScratch);
+  if (s.group == 64) return go_rows(distill_kernel<T, 64>, 64 + 32, a, s, smem, st);
+  return s.group == 128 ? go_rows(distill_kernel<T, 128>, 128 + 32, a, s, smem, st) : go_rows(distill_kernel<T, 256>, 256 + 32, a, s, smem, st);
 }
 template <typename T, int U, typename K> cudaError_t launch_grad(K kernel, GradArgs& a, cudaStream_t st) {
   a.segs = (logits_vectors(a.V, Elem<T>::E) + 32 * U - 1) / (32 * U);
@@ -1111,8 +1397,8 @@ fv_status fv_token_logprobs(const void* logits_dev, int32_t dtype, int64_t ld, i
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const double bytes = (double)rows * ((dtype ? 2.0 : 4.0) * V + 20.0 + 8.0 * n_alt);
   LaunchScope scope(KC_SELECT, 1, bytes, bytes, st);
-  RowsArgs a{logits_dev, ld, rows, V, 0, 0, 1.f / tau, ids_dev, n_alt, logprob_out_dev, reinterpret_cast<float2*>(stats_out_dev), entropy_out_dev,
-             alt_ids_out_dev, alt_logprob_out_dev, status_dev};
+  TokenArgs a{{logits_dev, ld, rows, V, 0, 0, 1.f / tau, status_dev}, ids_dev, n_alt, 0, logprob_out_dev, reinterpret_cast<float2*>(stats_out_dev), entropy_out_dev,
+              alt_ids_out_dev, alt_logprob_out_dev};
   return cu(dtype ? launch_token<__nv_bfloat16>(a, st) : launch_token<float>(a, st));
 }
 
@@ -1145,8 +1431,8 @@ fv_status fv_distill_topk(const void* logits_dev, int32_t dtype, int64_t ld, int
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const double bytes = (double)rows * ((dtype ? 2.0 : 4.0) * V * (dlogits_out_dev ? 2.0 : 1.0) + 8.0 * K + 16.0);
   LaunchScope scope(KC_SELECT, 1, bytes, bytes, st);
-  DistillArgs a{logits_dev, ld, rows, V, 0, 0, 1.f / tau, teacher_ids_dev, teacher_logits_dev, K, g_loss_dev, loss_out_dev, reinterpret_cast<float2*>(stats_out_dev),
-                dlogits_out_dev, ld_out, status_dev};
+  DistillArgs a{{logits_dev, ld, rows, V, 0, 0, 1.f / tau, status_dev}, teacher_ids_dev, teacher_logits_dev, K, g_loss_dev, loss_out_dev,
+                reinterpret_cast<float2*>(stats_out_dev), dlogits_out_dev, ld_out};
   return cu(dtype ? launch_distill<__nv_bfloat16>(a, st) : launch_distill<float>(a, st));
 }
 

@@ -247,12 +247,14 @@ def check_distill(x, t_ids, t_logits, g, tau, out=None):
     logq, q, _ = ref.teacher(t_ids, t_logits)
     lp = ref.logp.gather(1, t_ids.long().clamp(min=0))
     size = torch.where((q > 0) & torch.isfinite(lp), q * (logq.abs() + lp.abs()), torch.zeros_like(q)).sum(1)
-    near(r["loss"], loss, LN + U * 170 * (size + 1))
     want = ref.loss_grad(t_ids, t_logits, g)
     scale = torch.ones_like(loss) if g is None else g.double()
     tol = grad_tol(want, ref, scale, x.dtype) + (scale.abs() / tau * U * 170)[:, None] * (torch.zeros_like(want).scatter_add_(1, t_ids.long().clamp(min=0), q))
     fused = fv.fv_distill_topk(x, t_ids, t_logits, tau=tau, g_loss=g, want_grad=True)
-    assert torch.equal(fused["loss"].nan_to_num(nan=-1), r["loss"].nan_to_num(nan=-1)) and torch.equal(fused["stats"].nan_to_num(nan=-1), r["stats"].nan_to_num(nan=-1))
+    for one in (r, fused):               # (the loss alone and the loss with its gradient add in another order)
+        assert torch.equal(one["stats"][:, 0].double(), ref.m)
+        near(one["stats"][:, 1], ref.L, LN)
+        near(one["loss"], loss, LN + U * 170 * (size + 1))
     near(fused["dlogits"], want, tol)
     late = fv.fv_distill_topk_grad(x, t_ids, t_logits, r["stats"], g, tau=tau, out=out)
     near(late, want, tol)
