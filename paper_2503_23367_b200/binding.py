@@ -372,53 +372,75 @@ def fv_next_scale_input(r: torch.Tensor, h: int, w: int, h2: int, w2: int, w_in:
     return out
 
 
+_F32, _I32 = torch.float32, torch.int32
+
+
 def _rows(logits: torch.Tensor):
-    """(address, dtype code, row stride, rows, V) of a 2-D tensor of logits whose rows are contiguous, on the current device."""
-    assert logits.is_cuda and logits.dim() == 2 and (logits.stride(1) == 1 or logits.shape[1] == 1), "logits are [rows, V] CUDA tensors with contiguous rows"
-    assert logits.device.index == torch._C._cuda_getDevice(), "the logits are on another device than the current one"
-    dtype = logits.dtype
-    assert dtype == torch.float32 or dtype == torch.bfloat16, "logits are float32 or bfloat16"
+    """(address, dtype code, row stride, rows, V, device index) of a 2-D tensor of logits whose rows are contiguous, on the current device."""
+    assert logits.dim() == 2, "logits are [rows, V]"
     rows, V = logits.shape
-    return logits.data_ptr(), 1 if dtype == torch.bfloat16 else 0, logits.stride(0) if rows > 1 else V, rows, V
+    ld, step = logits.stride()
+    assert step == 1 or V == 1, "the rows of the logits are contiguous"
+    dev = logits.get_device()
+    assert dev == torch._C._cuda_getDevice(), "the logits are on the current CUDA device"
+    dtype = logits.dtype
+    assert dtype is _F32 or dtype is torch.bfloat16, "logits are float32 or bfloat16"
+    return logits.data_ptr(), 0 if dtype is _F32 else 1, ld if rows > 1 else V, rows, V, dev
 
 
-def _arg(t: Optional[torch.Tensor], dtype: torch.dtype, shape, like: torch.Tensor) -> Optional[int]:
-    """Address of a contiguous tensor of that type and shape on the logits' device, or None."""
+def _arg(t: Optional[torch.Tensor], dtype: torch.dtype, shape, dev: int) -> Optional[int]:
+    """Address of a contiguous tensor of that type and shape on that device, or None."""
     if t is None:
         return None
-    assert t.dtype == dtype and tuple(t.shape) == shape and t.device == like.device, f"expected {dtype} {list(shape)} on {like.device}"
-    return _ptr(t)
+    assert t.dtype is dtype and t.shape == shape and t.get_device() == dev and t.is_contiguous(), f"expected a contiguous {dtype} {list(shape)} on cuda:{dev}"
+    return t.data_ptr()
 
 
-def _grad_out(logits: torch.Tensor, out: Optional[torch.Tensor]):
-    """The tensor of a gradient of the logits: given, or new with the logits' row stride (rows then start at the same offset from 16 bytes)."""
+def _new(n: int, like: torch.Tensor, dtype=_F32) -> torch.Tensor:
+    return torch.empty_strided((n,), (1,), dtype=dtype, device=like.device)
+
+
+def _new2(n: int, m: int, like: torch.Tensor, dtype=_F32) -> torch.Tensor:
+    return torch.empty_strided((n, m), (m, 1), dtype=dtype, device=like.device)
+
+
+def _grad_out(logits: torch.Tensor, ld: int, dev: int, out: Optional[torch.Tensor]):
+    """The tensor of a gradient of the logits: given, or new with the logits' row stride (its rows then start at the same offsets from 16 bytes)."""
+    rows, V = logits.shape
     if out is None:
-        rows, V = logits.shape
-        ld = max(V, logits.stride(0)) if rows > 1 else V
+        ld = max(ld, V)
         pad = (logits.data_ptr() & 15) // logits.element_size()
-        out = _empty((pad + rows * ld,), logits.dtype, logits.device).as_strided((rows, V), (ld, 1), pad)
-    assert out.dtype == logits.dtype and out.shape == logits.shape and out.device == logits.device and (out.stride(1) == 1 or out.shape[1] == 1)
-    return out, out.data_ptr(), out.stride(0) if out.shape[0] > 1 else out.shape[1]
+        if pad:
+            out = torch.empty_strided((pad + rows * ld,), (1,), dtype=logits.dtype, device=logits.device).as_strided((rows, V), (ld, 1), pad)
+        else:
+            out = torch.empty_strided((rows, V), (ld, 1), dtype=logits.dtype, device=logits.device)
+        return out, out.data_ptr(), ld
+    ldo, step = out.stride()
+    assert out.dtype is logits.dtype and out.shape == logits.shape and out.get_device() == dev and (step == 1 or V == 1), "a gradient has the type, shape and device of the logits, its rows contiguous"
+    return out, out.data_ptr(), ldo if rows > 1 else V
 
 
 def fv_token_logprobs(logits: torch.Tensor, ids: Optional[torch.Tensor] = None, tau: float = 1.0, n_alt: int = 0,
                       want_entropy: bool = False, status: Optional[torch.Tensor] = None) -> dict:
     """logits [rows, V] fp32 or bf16 -> {"stats" [rows, 2] (m, L), "logprob" [rows] of ids (int32, -1 = none), "entropy" [rows],
     "alt_ids" int32 / "alt_logprob" [rows, n_alt]}, the last three where asked for."""
-    x, dt, ld, rows, V = _rows(logits)
-    dev = logits.device
-    r = {"stats": _empty((rows, 2), torch.float32, dev)}
-    idp = _arg(ids, torch.int32, (rows,), logits)
+    x, dt, ld, rows, V, dev = _rows(logits)
+    stats = _new2(rows, 2, logits)
+    r = {"stats": stats}
+    idp = lpp = entp = altp = altlp = None
     if ids is not None:
-        r["logprob"] = _empty((rows,), torch.float32, dev)
+        idp = _arg(ids, _I32, (rows,), dev)
+        r["logprob"] = lp = _new(rows, logits)
+        lpp = lp.data_ptr()
     if want_entropy:
-        r["entropy"] = _empty((rows,), torch.float32, dev)
-    if n_alt:
-        r["alt_ids"] = _empty((rows, max(n_alt, 0)), torch.int32, dev)
-        r["alt_logprob"] = _empty((rows, max(n_alt, 0)), torch.float32, dev)
-    at = lambda k: r[k].data_ptr() if k in r else None
-    _check(lib().fv_token_logprobs(x, dt, ld, rows, V, tau, idp, n_alt, at("logprob"), at("stats"), at("entropy"), at("alt_ids"),
-                                   at("alt_logprob"), _ptr(status), _stream()), "fv_token_logprobs")
+        r["entropy"] = ent = _new(rows, logits)
+        entp = ent.data_ptr()
+    if n_alt > 0:
+        r["alt_ids"] = alt = _new2(rows, n_alt, logits, _I32)
+        r["alt_logprob"] = altl = _new2(rows, n_alt, logits)
+        altp, altlp = alt.data_ptr(), altl.data_ptr()
+    _check(lib().fv_token_logprobs(x, dt, ld, rows, V, tau, idp, n_alt, lpp, stats.data_ptr(), entp, altp, altlp, _ptr(status), _stream()),
+           "fv_token_logprobs")
     return r
 
 
@@ -426,12 +448,12 @@ def fv_token_logprobs_grad(logits: torch.Tensor, ids: Optional[torch.Tensor], st
                            tau: float = 1.0, entropy: Optional[torch.Tensor] = None, g_entropy: Optional[torch.Tensor] = None,
                            out: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Gradient of sum_r g_logprob[r] logprob[r] + g_entropy[r] entropy[r] by the logits; out may be the logits themselves."""
-    x, dt, ld, rows, V = _rows(logits)
-    out, op, ldo = _grad_out(logits, out)
-    f32 = torch.float32
-    _check(lib().fv_token_logprobs_grad(x, dt, ld, rows, V, tau, _arg(ids, torch.int32, (rows,), logits), _arg(stats, f32, (rows, 2), logits),
-                                        _arg(entropy, f32, (rows,), logits), _arg(g_logprob, f32, (rows,), logits),
-                                        _arg(g_entropy, f32, (rows,), logits), op, ldo, _ptr(status), _stream()), "fv_token_logprobs_grad")
+    x, dt, ld, rows, V, dev = _rows(logits)
+    out, op, ldo = _grad_out(logits, ld, dev, out)
+    one = (rows,)
+    _check(lib().fv_token_logprobs_grad(x, dt, ld, rows, V, tau, _arg(ids, _I32, one, dev), _arg(stats, _F32, (rows, 2), dev), _arg(entropy, _F32, one, dev),
+                                        _arg(g_logprob, _F32, one, dev), _arg(g_entropy, _F32, one, dev), op, ldo, _ptr(status), _stream()),
+           "fv_token_logprobs_grad")
     return out
 
 
@@ -440,15 +462,15 @@ def fv_distill_topk(logits: torch.Tensor, teacher_ids: torch.Tensor, teacher_log
                     status: Optional[torch.Tensor] = None) -> dict:
     """Loss per row against a teacher's top logits ([rows, K], ids int32, -1 = no entry): {"loss" [rows], "stats" [rows, 2]} and, with
     want_grad, "dlogits" = g_loss[r] * its gradient (g_loss None: 1) from the same pass; out may be the logits themselves."""
-    x, dt, ld, rows, V = _rows(logits)
+    x, dt, ld, rows, V, dev = _rows(logits)
     K = teacher_ids.shape[-1]
-    dev, f32 = logits.device, torch.float32
-    r = {"loss": _empty((rows,), f32, dev), "stats": _empty((rows, 2), f32, dev)}
+    loss, stats = _new(rows, logits), _new2(rows, 2, logits)
+    r = {"loss": loss, "stats": stats}
     op, ldo = None, 0
     if want_grad:
-        r["dlogits"], op, ldo = _grad_out(logits, out)
-    _check(lib().fv_distill_topk(x, dt, ld, rows, V, tau, _arg(teacher_ids, torch.int32, (rows, K), logits), _arg(teacher_logits, f32, (rows, K), logits), K,
-                                 _arg(g_loss, f32, (rows,), logits), r["loss"].data_ptr(), r["stats"].data_ptr(), op, ldo, _ptr(status), _stream()), "fv_distill_topk")
+        r["dlogits"], op, ldo = _grad_out(logits, ld, dev, out)
+    _check(lib().fv_distill_topk(x, dt, ld, rows, V, tau, _arg(teacher_ids, _I32, (rows, K), dev), _arg(teacher_logits, _F32, (rows, K), dev), K,
+                                 _arg(g_loss, _F32, (rows,), dev), loss.data_ptr(), stats.data_ptr(), op, ldo, _ptr(status), _stream()), "fv_distill_topk")
     return r
 
 
@@ -456,12 +478,11 @@ def fv_distill_topk_grad(logits: torch.Tensor, teacher_ids: torch.Tensor, teache
                          g_loss: Optional[torch.Tensor] = None, tau: float = 1.0, out: Optional[torch.Tensor] = None,
                          status: Optional[torch.Tensor] = None) -> torch.Tensor:
     """g_loss[r] * gradient of fv_distill_topk's loss by the logits, from the stats it left; out may be the logits themselves."""
-    x, dt, ld, rows, V = _rows(logits)
+    x, dt, ld, rows, V, dev = _rows(logits)
     K = teacher_ids.shape[-1]
-    out, op, ldo = _grad_out(logits, out)
-    f32 = torch.float32
-    _check(lib().fv_distill_topk_grad(x, dt, ld, rows, V, tau, _arg(teacher_ids, torch.int32, (rows, K), logits), _arg(teacher_logits, f32, (rows, K), logits), K,
-                                      _arg(stats, f32, (rows, 2), logits), _arg(g_loss, f32, (rows,), logits), op, ldo, _ptr(status), _stream()), "fv_distill_topk_grad")
+    out, op, ldo = _grad_out(logits, ld, dev, out)
+    _check(lib().fv_distill_topk_grad(x, dt, ld, rows, V, tau, _arg(teacher_ids, _I32, (rows, K), dev), _arg(teacher_logits, _F32, (rows, K), dev), K,
+                                      _arg(stats, _F32, (rows, 2), dev), _arg(g_loss, _F32, (rows,), dev), op, ldo, _ptr(status), _stream()), "fv_distill_topk_grad")
     return out
 
 
@@ -470,18 +491,22 @@ def fv_linear_logprobs(a: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Te
     """As fv_token_logprobs on the rows a [rows, C] * w [V, C]^T + bias [V] (all bf16), whose logits are not kept."""
     rows, Cw = a.shape
     V = w.shape[0]
-    assert a.dtype == torch.bfloat16 and a.is_cuda and a.device.index == torch._C._cuda_getDevice()
-    bf, dev, f32 = torch.bfloat16, a.device, torch.float32
+    dev, bf = a.get_device(), torch.bfloat16
+    assert dev == torch._C._cuda_getDevice(), "the rows are on the current CUDA device"
+    ap, wp, bp, idp = _arg(a, bf, (rows, Cw), dev), _arg(w, bf, (V, Cw), dev), _arg(bias, bf, (V,), dev), _arg(ids, _I32, (rows,), dev)
     ws_bytes = lib().fv_linear_logprobs_workspace_bytes(rows, V)
-    ws = _empty((ws_bytes + 256,), torch.uint8, dev)
-    r = {"stats": _empty((rows, 2), f32, dev)}
+    ws = _new(ws_bytes + 256, a, torch.uint8)
+    stats = _new2(rows, 2, a)
+    r = {"stats": stats}
+    lpp = entp = None
     if ids is not None:
-        r["logprob"] = _empty((rows,), f32, dev)
+        r["logprob"] = lp = _new(rows, a)
+        lpp = lp.data_ptr()
     if want_entropy:
-        r["entropy"] = _empty((rows,), f32, dev)
-    at = lambda k: r[k].data_ptr() if k in r else None
-    _check(lib().fv_linear_logprobs(_ptr(a), _arg(w, bf, (V, Cw), a), _arg(bias, bf, (V,), a), rows, Cw, V, tau, _arg(ids, torch.int32, (rows,), a),
-                                    at("logprob"), at("stats"), at("entropy"), (ws.data_ptr() + 255) // 256 * 256, ws_bytes, _ptr(status), _stream()), "fv_linear_logprobs")
+        r["entropy"] = ent = _new(rows, a)
+        entp = ent.data_ptr()
+    _check(lib().fv_linear_logprobs(ap, wp, bp, rows, Cw, V, tau, idp, lpp, stats.data_ptr(), entp, (ws.data_ptr() + 255) // 256 * 256, ws_bytes, _ptr(status), _stream()),
+           "fv_linear_logprobs")
     return r
 
 
