@@ -18,53 +18,18 @@
 #include <type_traits>
 
 #include "internal.h"
+#include "logits.cuh"
 #include "sm100.cuh"   // the device status codes, cluster barriers
 
 namespace fv {
+
+using namespace logits_detail;
+
 namespace {
 
 constexpr int kMaxAlt = 64;        // alternatives of a row
 constexpr int kMaxTeacher = 128;   // entries of a teacher's row
 constexpr int kMaxCluster = 8;     // CTAs that share a row
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-
-// ---- small pieces -----------------------------------------------------------------------------------------------------
-__device__ __forceinline__ float exp2_fast(float x) {   // 2^x within 2^-22 of its value, 0 at -inf, NaN at NaN
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-__device__ __forceinline__ uint64_t pack2(float lo, float hi) {
-  uint64_t r;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
-  return r;
-}
-__device__ __forceinline__ void unpack2(uint64_t v, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
-__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
-  uint64_t r;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-  return r;
-}
-__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
-  uint64_t r;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-  return r;
-}
-__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
-  uint64_t r;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-  return r;
-}
-__device__ __forceinline__ float warp_max(float v) {   // (no NaN comes here)
-  float r;
-  asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
-  return r;
-}
-__device__ __forceinline__ float warp_sum(float v) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
-  return v;
-}
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
@@ -77,10 +42,6 @@ __device__ __forceinline__ uint32_t peer_smem(const void* p, uint32_t cta) {   /
 __device__ __forceinline__ void peer_store(uint32_t addr, float v) { asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(addr), "f"(v) : "memory"); }
 __device__ __forceinline__ void peer_store(uint32_t addr, int v) { asm volatile("st.shared::cluster.s32 [%0], %1;" ::"r"(addr), "r"(v) : "memory"); }
 __device__ __forceinline__ void peer_store(uint32_t addr, uint64_t v) { asm volatile("st.shared::cluster.b64 [%0], %1;" ::"r"(addr), "l"(v) : "memory"); }
-__device__ __forceinline__ void put_status(int32_t* status, int code) {
-  if (status) atomicCAS(status, 0, code);
-}
-
 // fp32 and bf16 logits: E elements in a 16-byte vector.
 template <typename T> struct Elem;
 template <> struct Elem<float> {
@@ -210,30 +171,6 @@ template <typename T, int G> struct Slice {
   }
 };
 
-// ---- exponents ---------------------------------------------------------------------------------------------------------------
-// e = 2^d, d = (x - m) c, c = log2(e) / tau.  Near 0 (|m c| < 2^21) d is taken as x c - R in one operation, R the whole number next to m c (or to that of an
-// earlier maximum): R is exact, so all of a row's exponents are off by the one number m c - R, by which the sums are put right (delta).  That saves
-// half an instruction per logit.  Far from 0, where x c has no fraction left (masks of -1e9, of the type's lowest value), the difference is taken first.
-constexpr float kFar = 2097152.f;      // 2^21
-__device__ __forceinline__ float safe_max(float m) { return m == -INFINITY ? 0.f : m; }
-__device__ __forceinline__ bool is_near(float m, float c) { return fabsf(m * c) < kFar; }
-__device__ __forceinline__ float whole_ref(float m, float c) { return fmaxf(rintf(m * c), -2.f * kFar); }   // a thread far below the row's maximum adds nothing
-__device__ __forceinline__ float delta(float m, float c, float R) { return fmaf(-m, c, R); }   // d from m less d from R
-template <bool NEAR> struct Expo {
-  uint64_t a, b;
-  __device__ __forceinline__ Expo(float ref, float c) : a(pack2(c, c)), b(pack2(-ref, -ref)) {}   // ref: R near, m far
-  __device__ __forceinline__ uint64_t operator()(uint64_t x) const { return NEAR ? fma2(x, a, b) : mul2(add2(x, b), a); }
-};
-__device__ __forceinline__ uint64_t exp2_pair(uint64_t d) {
-  float a, b;
-  unpack2(d, a, b);
-  return pack2(exp2_fast(a), exp2_fast(b));
-}
-__device__ __forceinline__ float sum_pair(uint64_t v) {
-  float a, b;
-  unpack2(v, a, b);
-  return a + b;
-}
 // s = sum e and t = sum e d over vectors of logits.
 template <typename T, bool ENT> struct Sums {
   uint64_t s[2] = {0, 0}, t[2] = {0, 0};
@@ -254,37 +191,6 @@ template <typename T, bool ENT> struct Sums {
   }
 };
 
-// What the parts of a row know of it, and what the whole row comes to.
-struct Part { float m, s, t; };
-struct Stat { float m, L, H, s; };
-// Sums whose exponents were too small by delta, against m.
-template <typename S> __device__ __forceinline__ Part part_of(float m, const S& sums, float delta) {
-  const float s = sum_pair(add2(sums.s[0], sums.s[1])), t = sum_pair(add2(sums.t[0], sums.t[1]));
-  if (s == 0.f) return {m, 0.f, 0.f};
-  const float f = exp2_fast(delta);
-  return {m, s * f, fmaf(delta, s, t) * f};
-}
-template <bool ENT> __device__ __forceinline__ Stat stat_of(float m, float s, float t) {
-  if (s > 0.f && s < 1.f) s = 1.f;      // rounding: the largest logit alone adds 1, and no log probability is above 0
-  Stat r{m, logf(s), 0.f, s};
-  if (ENT && s != 0.f) {
-    r.H = r.L - kLn2 * (t / s);
-    if (r.H < 0.f) r.H = 0.f;
-  }
-  return r;
-}
-// Two sets of elements, each with its sums against its own maximum, against a common one.  s = 0: nothing but -inf, its maximum means nothing.
-template <bool ENT> __device__ __forceinline__ Part against(const Part& p, float m, float c) {
-  const float up = (safe_max(p.m) - safe_max(m)) * c, f = p.s == 0.f ? 0.f : exp2_fast(up);
-  return {m, p.s * f, ENT && f != 0.f ? fmaf(p.s, up, p.t) * f : 0.f};
-}
-// The union of a warp's sets, in every lane.
-template <bool ENT> __device__ __forceinline__ Part warp_union(const Part& mine, float c) {
-  Part r = against<ENT>(mine, warp_max(mine.m), c);
-  r.s = warp_sum(r.s);
-  if (ENT) r.t = warp_sum(r.t);
-  return r;
-}
 // The whole row from its parts, one of each warp that went over it (at most 64), by a whole warp.
 template <bool ENT> __device__ __forceinline__ Stat stat_of_parts(const Part* parts, int n, float c, int lane) {
   Part p{-INFINITY, 0.f, 0.f};
@@ -1323,13 +1229,10 @@ template <typename T> cudaError_t allow_all() {
 // Function attributes belong to a device: set on the first call on each.
 cudaError_t logits_init() {
   static std::atomic<uint64_t> done{0};
-  int dev = 0;
-  cudaError_t e = cudaGetDevice(&dev);
-  if (e != cudaSuccess || (dev < 64 && (done.load(std::memory_order_acquire) >> dev & 1))) return e;
-  e = allow_all<float>();
-  if (e == cudaSuccess) e = allow_all<__nv_bfloat16>();
-  if (e == cudaSuccess && dev < 64) done.fetch_or(1ull << dev, std::memory_order_release);
-  return e;
+  return once_per_device(done, [] {
+    const cudaError_t e = allow_all<float>();
+    return e == cudaSuccess ? allow_all<__nv_bfloat16>() : e;
+  });
 }
 
 template <typename K, typename A> cudaError_t go_rows(K kernel, int threads, A& a, const Shape& s, size_t smem, cudaStream_t st) {
@@ -1449,21 +1352,6 @@ fv_status fv_distill_topk_grad(const void* logits_dev, int32_t dtype, int64_t ld
   GradArgs a{logits_dev, ld, rows, V, 0, 1.f / tau, reinterpret_cast<const float2*>(stats_dev), nullptr, nullptr, g_loss_dev, nullptr,
              teacher_ids_dev, teacher_logits_dev, K, dlogits_out_dev, ld_out, status_dev};
   return cu(dtype ? launch_grad<__nv_bfloat16, 8>(distill_grad_kernel<__nv_bfloat16, 8>, a, st) : launch_grad<float, 8>(distill_grad_kernel<float, 8>, a, st));
-}
-
-size_t fv_linear_logprobs_workspace_bytes(int32_t rows, int32_t V) {
-  if (rows <= 0 || V <= 0) return 0;
-  return align_up((size_t)rows * V * 4, 256);
-}
-
-fv_status fv_linear_logprobs(const void* a_dev, const void* w_dev, const void* bias_dev, int32_t rows, int32_t C, int32_t V, float tau, const int32_t* ids_dev,
-                             float* logprob_out_dev, float* stats_out_dev, float* entropy_out_dev, void* workspace_dev, size_t workspace_bytes, int32_t* status_dev,
-                             void* stream) {
-  if (!workspace_dev || !al(workspace_dev, 256)) return FV_ERR_INVALID_ARG;
-  if (workspace_bytes < fv_linear_logprobs_workspace_bytes(rows, V)) return FV_ERR_CAPACITY;
-  const fv_status s = fv_gemm_bf16(a_dev, w_dev, bias_dev, rows, V, C, EPI_F32, workspace_dev, nullptr, nullptr, 0, rows, status_dev, nullptr, 0, stream);
-  if (s != FV_OK) return s;
-  return fv_token_logprobs(workspace_dev, 0, V, rows, V, tau, ids_dev, 0, logprob_out_dev, stats_out_dev, entropy_out_dev, nullptr, nullptr, status_dev, stream);
 }
 
 }  // extern "C"
