@@ -30,6 +30,12 @@ namespace {
 constexpr int kMaxAlt = 64;        // alternatives of a row
 constexpr int kMaxTeacher = 128;   // entries of a teacher's row
 constexpr int kMaxCluster = 8;     // CTAs that share a row
+// Read once: first to leave the caches (and, like dep_load16, it stays where it is written).
+__device__ __forceinline__ uint4 load16_once(const void* p) {
+  uint4 v;
+  asm volatile("ld.global.cs.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+  return v;
+}
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
@@ -464,12 +470,18 @@ template <typename T, int G> __device__ __forceinline__ void warp_select(const S
     f.add<T>(u, mine ? reach_bits<T>(u, thr) : 0, st.part * Elem<T>::E - st.off);
   }
   int h = 0;
-  for (int k = 0; k < turns; ++k) {
-    const bool hit = bm[k * 32 + lane] >= thr;
-    const uint32_t who = __ballot_sync(0xFFFFFFFFu, hit);
-    const int at = h + __popc(who & below);
-    if (hit && at < kMaxCand) wa.hit[at] = (uint16_t)(k * 32 + lane);
-    h += __popc(who);
+  for (int k0 = 0; k0 < turns; k0 += 4) {
+    float b[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) b[i] = k0 + i < turns ? bm[(k0 + i) * 32 + lane] : -INFINITY;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const bool hit = b[i] >= thr;
+      const uint32_t who = __ballot_sync(0xFFFFFFFFu, hit);
+      const int at = h + __popc(who & below);
+      if (hit && at < kMaxCand) wa.hit[at] = (uint16_t)((k0 + i) * 32 + lane);
+      h += __popc(who);
+    }
   }
   __syncwarp();
   bool fits = h <= kMaxCand;
@@ -673,18 +685,19 @@ __global__ void __launch_bounds__(kStreamThreads, 8) token_logprobs_kernel(const
     const Stat stat = stat_of_parts<ENT>(sh.part[near ? 0 : 1], warps, c, lane);
     if constexpr (ALT) {               // every key's place is how many are larger
       const int per = kStreamThreads / warps, l = threadIdx.x / per;   // threads of a list; this thread's
-      int total = 0;
-      for (int i = 0; i < warps; ++i) total += ra.count[i];
-      for (int i = threadIdx.x % per; i < ra.count[l]; i += per) {
-        const unsigned long long key = lists[(size_t)l * p.n_alt + i];
+      const int have = lane < warps ? ra.count[lane] : 0, total = __reduce_add_sync(0xFFFFFFFFu, have);
+      const int mine_n = __shfl_sync(0xFFFFFFFFu, have, l);
+      for (int i0 = 0; __any_sync(0xFFFFFFFFu, i0 + (int)threadIdx.x % per < mine_n); i0 += per) {
+        const int i = i0 + threadIdx.x % per;
+        const unsigned long long key = i < mine_n ? lists[(size_t)l * p.n_alt + i] : ~0ull;
         int place = 0;
-        for (int o = 0; o < warps; ++o) {
+        for (uint32_t left = __ballot_sync(0xFFFFFFFFu, have > 0); left; left &= left - 1) {
+          const int o = __ffs(left) - 1, n = __shfl_sync(0xFFFFFFFFu, have, o);
           const unsigned long long* k = lists + (size_t)o * p.n_alt;
-          const int n = ra.count[o];
-#pragma unroll 4
+#pragma unroll 8
           for (int j = 0; j < n; ++j) place += k[j] > key;
         }
-        if (place < p.n_alt) tell_alt<ENT>(p, row, stat, place, key);
+        if (i < mine_n && place < p.n_alt) tell_alt<ENT>(p, row, stat, place, key);
       }
       if ((int)threadIdx.x >= total && (int)threadIdx.x < p.n_alt) tell_alt<ENT>(p, row, stat, threadIdx.x, 0ull);
     }
@@ -829,7 +842,7 @@ template <typename T, int G, typename F> __device__ __forceinline__ void write_r
 #pragma unroll
     for (int i = 0; i < P; ++i) d[i] = f(d[i]);
     if (vec && sl.whole(v)) {
-      *reinterpret_cast<uint4*>(dvec + (size_t)v * E) = Elem<T>::pack(d);
+      __stcs(reinterpret_cast<uint4*>(dvec + (size_t)v * E), Elem<T>::pack(d));
     } else {
       const int i0 = sl.first_index(v);
 #pragma unroll
@@ -994,7 +1007,7 @@ struct GradArgs {
   void* dx; long long ld_dx;
   int32_t* status;
 };
-constexpr int kGradWarps = 8;
+constexpr int kGradWarps = 4, UB = 4, UF = 4, UD = 8;
 
 // The part of a row that a warp takes: where its vectors lie, what they hold, how they are written.
 template <typename T, int U> struct Segment {
@@ -1016,7 +1029,7 @@ template <typename T, int U> struct Segment {
     for (int u = 0; u < U; ++u) {
       const int i0 = first_index(u);
       if (whole(u)) {
-        x[u] = dep_load16(row + i0);
+        x[u] = load16_once(row + i0);
       } else if (v0 + 32 * u < nv) {
         uint64_t f[E / 2];
 #pragma unroll
@@ -1029,7 +1042,7 @@ template <typename T, int U> struct Segment {
   __device__ __forceinline__ void store(int u, const uint64_t (&d)[E / 2]) const {
     const int i0 = first_index(u);
     if (vec && whole(u)) {
-      *reinterpret_cast<uint4*>(drow + i0) = Elem<T>::pack(d);
+      __stcs(reinterpret_cast<uint4*>(drow + i0), Elem<T>::pack(d));
     } else {
 #pragma unroll
       for (int e = 0; e < E; ++e) {
@@ -1319,8 +1332,8 @@ fv_status fv_token_logprobs_grad(const void* logits_dev, int32_t dtype, int64_t 
   GradArgs a{logits_dev, ld, rows, V, 0, 1.f / tau, reinterpret_cast<const float2*>(stats_dev), entropy_dev, ids_dev, g_logprob_dev, g_entropy_dev,
              nullptr, nullptr, 0, dlogits_out_dev, ld_out, status_dev};
   using B = __nv_bfloat16;
-  if (dtype) return cu(g_entropy_dev ? launch_grad<B, 4>(token_logprobs_grad_kernel<B, 4, true>, a, st) : launch_grad<B, 4>(token_logprobs_grad_kernel<B, 4, false>, a, st));
-  return cu(g_entropy_dev ? launch_grad<float, 4>(token_logprobs_grad_kernel<float, 4, true>, a, st) : launch_grad<float, 4>(token_logprobs_grad_kernel<float, 4, false>, a, st));
+  if (dtype) return cu(g_entropy_dev ? launch_grad<B, UB>(token_logprobs_grad_kernel<B, UB, true>, a, st) : launch_grad<B, UB>(token_logprobs_grad_kernel<B, UB, false>, a, st));
+  return cu(g_entropy_dev ? launch_grad<float, UF>(token_logprobs_grad_kernel<float, UF, true>, a, st) : launch_grad<float, UF>(token_logprobs_grad_kernel<float, UF, false>, a, st));
 }
 
 fv_status fv_distill_topk(const void* logits_dev, int32_t dtype, int64_t ld, int32_t rows, int32_t V, float tau, const int32_t* teacher_ids_dev,
@@ -1351,7 +1364,7 @@ fv_status fv_distill_topk_grad(const void* logits_dev, int32_t dtype, int64_t ld
   LaunchScope scope(KC_SELECT, 1, bytes, bytes, st);
   GradArgs a{logits_dev, ld, rows, V, 0, 1.f / tau, reinterpret_cast<const float2*>(stats_dev), nullptr, nullptr, g_loss_dev, nullptr,
              teacher_ids_dev, teacher_logits_dev, K, dlogits_out_dev, ld_out, status_dev};
-  return cu(dtype ? launch_grad<__nv_bfloat16, 8>(distill_grad_kernel<__nv_bfloat16, 8>, a, st) : launch_grad<float, 8>(distill_grad_kernel<float, 8>, a, st));
+  return cu(dtype ? launch_grad<__nv_bfloat16, UD>(distill_grad_kernel<__nv_bfloat16, UD>, a, st) : launch_grad<float, UD>(distill_grad_kernel<float, UD>, a, st));
 }
 
 }  // extern "C"
