@@ -11,6 +11,7 @@
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
+#include <algorithm>
 #include <atomic>
 #include <climits>
 #include <type_traits>
@@ -249,8 +250,9 @@ linear_logprobs_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
   }
 }
 
-// The row's parts put together: a CTA has 32 rows, one per lane; its warps take the parts in turn.
-constexpr int kFinishWarps = 8;
+// The row's parts put together.  A CTA has R rows, neighbouring threads neighbouring rows; its 256 / R threads of a row take the parts in turn.  32 rows where there are
+// few parts; 8 where there are many, of which a thread would else read a long chain (300 rows of 512 parts: 24 us beside the product with 32 rows, 4 with 8).
+constexpr int kFinishThreads = 256, kFinishWarps = kFinishThreads / 32, kManyParts = 64;
 struct FinishArgs {
   const float4* part; const float* xid; const int32_t* ids;
   int M, N, parts;
@@ -258,10 +260,11 @@ struct FinishArgs {
   float* logprob; float2* stats; float* entropy;
   int32_t* status;
 };
-__global__ void __launch_bounds__(32 * kFinishWarps) linear_finish_kernel(const FinishArgs p) {
-  __shared__ Part all[kFinishWarps][32];
+template <int R> __global__ void __launch_bounds__(kFinishThreads) linear_finish_kernel(const FinishArgs p) {
+  constexpr int PER = kFinishThreads / R;          // threads of a row
+  __shared__ Part all[kFinishWarps][R];
   pdl_trigger();
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, row = blockIdx.x * 32 + lane;
+  const int warp = threadIdx.x >> 5, r = threadIdx.x % R, row = blockIdx.x * R + r;
   const bool row_ok = row < p.M;
   pdl_wait();
   const auto join = [&](const Part& a, const Part& b) {
@@ -270,20 +273,24 @@ __global__ void __launch_bounds__(32 * kFinishWarps) linear_finish_kernel(const 
     return Part{m, x.s + y.s, x.t + y.t};
   };
   Part mine{-INFINITY, 0.f, 0.f};
-  for (int i = warp; row_ok && i < p.parts; i += 4 * kFinishWarps) {
+  for (int i = threadIdx.x / R; row_ok && i < p.parts; i += 4 * PER) {
     float4 v[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j)
-      if (i + j * kFinishWarps < p.parts) v[j] = dep_load4(p.part + (size_t)(i + j * kFinishWarps) * p.M + row);
+      if (i + j * PER < p.parts) v[j] = dep_load4(p.part + (size_t)(i + j * PER) * p.M + row);
 #pragma unroll
     for (int j = 0; j < 4; ++j)
-      if (i + j * kFinishWarps < p.parts) mine = join(mine, Part{v[j].x, v[j].y, v[j].z});
+      if (i + j * PER < p.parts) mine = join(mine, Part{v[j].x, v[j].y, v[j].z});
   }
-  all[warp][lane] = mine;
-  __syncthreads();
-  if (warp != 0 || !row_ok) return;
+  __syncwarp();
 #pragma unroll
-  for (int w = 1; w < kFinishWarps; ++w) mine = join(mine, all[w][lane]);
+  for (int o = 16; o >= R; o >>= 1)
+    mine = join(mine, Part{__shfl_xor_sync(0xFFFFFFFFu, mine.m, o), __shfl_xor_sync(0xFFFFFFFFu, mine.s, o), __shfl_xor_sync(0xFFFFFFFFu, mine.t, o)});
+  if ((threadIdx.x & 31) < R) all[warp][r] = mine;
+  __syncthreads();
+  if (threadIdx.x >= R || !row_ok) return;
+#pragma unroll
+  for (int w = 1; w < kFinishWarps; ++w) mine = join(mine, all[w][r]);
   const Stat st = stat_of<true>(mine.m, mine.s, mine.t);
   if (p.stats) p.stats[row] = make_float2(st.m, st.L);
   if (p.entropy) p.entropy[row] = st.H;
@@ -291,7 +298,7 @@ __global__ void __launch_bounds__(32 * kFinishWarps) linear_finish_kernel(const 
   const int id = dep_load(p.ids + row);
   float lp = 0.f;
   if (id >= 0 && id < p.N) {
-    lp = (dep_load(p.xid + row) - st.m) * p.inv_tau - st.L;
+    lp = st.L == -INFINITY ? -INFINITY : (dep_load(p.xid + row) - st.m) * p.inv_tau - st.L;   // (a bias may forbid tokens)
   } else if (id != -1) {
     put_status(p.status, DEV_BAD_TOKEN_ID);
     lp = __int_as_float(0x7FC00000);
@@ -299,27 +306,21 @@ __global__ void __launch_bounds__(32 * kFinishWarps) linear_finish_kernel(const 
   p.logprob[row] = lp;
 }
 
-// Tile width: the cheapest by rounds x (a round's own cost + k-blocks x a block's), in the units of the GEMM's fits (gemm_choice.h; the 64-wide pair from its own).
-int pick_width(int M, int N, int K, int pairs) {
-  const struct { int bn; double round_us, kb_us; } cand[3] = {{256, 1.55, 0.292}, {128, 1.11, 0.168}, {64, 0.9, 0.13}};
-  int best = 256;
-  double best_cost = 1e30;
-  for (const auto& c : cand) {
-    const long tiles = (long)((M + 2 * BM - 1) / (2 * BM)) * ((N + c.bn - 1) / c.bn);
-    const double cost = (double)((tiles + pairs - 1) / pairs) * (c.round_us + (K + BK - 1) / BK * c.kb_us);
-    if (cost < best_cost - 1e-9) { best_cost = cost; best = c.bn; }
-  }
-  return best;
+// Tile width: the cheaper by rounds, one of 128 columns costing 0.62 of one of 256 (us, 256 / 128 wide: 400 rows, C 2048, V 4096 17.6 / 13.2; 820 18.7 / 22.0; 5000, C 256,
+// V 1000 15.1 / 13.3; 8192, C 2048, V 4096 93 / 113; tiles of 64 columns were never faster).
+int tile_width(int M, int N) {
+  const auto rounds = [&](int bn) { return (((long)(M + 2 * BM - 1) / (2 * BM)) * ((N + bn - 1) / bn) + 73) / 74; };
+  return 0.62 * rounds(128) < rounds(256) ? 128 : 256;
 }
+int column_parts(int M, int N) { const int bn = tile_width(M, N); return 2 * ((N + bn - 1) / bn); }
 
 template <int BN> cudaError_t allow_smem() { return cudaFuncSetAttribute(linear_logprobs_kernel<BN>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<BN>::kSmem); }
 // Function attributes belong to a device: set on the first call on each.
 cudaError_t linear_init() {
   static std::atomic<uint64_t> done{0};
   return once_per_device(done, [] {
-    cudaError_t e = allow_smem<256>();
-    if (e == cudaSuccess) e = allow_smem<128>();
-    return e == cudaSuccess ? allow_smem<64>() : e;
+    const cudaError_t e = allow_smem<256>();
+    return e == cudaSuccess ? allow_smem<128>() : e;
   });
 }
 
@@ -331,7 +332,10 @@ template <int BN> cudaError_t launch_width(const void* a, const void* w, const L
   return launch_pdl(linear_logprobs_kernel<BN>, dim3(2 * pairs), dim3(kThreads), Cfg<BN>::kSmem, st, tmA, tmB, p);
 }
 
-int column_parts(int V) { return 2 * ((V + 63) / 64); }   // most that any width makes
+// Few rows: the product with K split over a cluster (fv_gemm_bf16; its slices are at most 512 of K for these sizes, so its sums are as exact) and the rows read back from
+// L2, which is sooner done than 256-row tiles (one row, C 1024, V 4096: 10.8 -> 6 us).
+constexpr int kFewRows = 48, kFewColumns = 9472, kFewK = 2048;
+size_t few_rows_bytes(int rows, int V) { return rows <= kFewRows && V <= kFewColumns ? (size_t)rows * V * 4 : 0; }
 
 bool aligned_to(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 
@@ -344,32 +348,40 @@ extern "C" {
 
 size_t fv_linear_logprobs_workspace_bytes(int32_t rows, int32_t V) {
   if (rows <= 0 || V <= 0) return 0;
-  return align_up((size_t)rows * column_parts(V) * sizeof(float4), 256) + align_up((size_t)rows * 4, 256);
+  const size_t parts = align_up((size_t)rows * column_parts(rows, V) * sizeof(float4), 256) + align_up((size_t)rows * 4, 256);
+  return std::max(parts, align_up(few_rows_bytes(rows, V), 256));
 }
 
 fv_status fv_linear_logprobs(const void* a_dev, const void* w_dev, const void* bias_dev, int32_t rows, int32_t C, int32_t V, float tau, const int32_t* ids_dev,
                              float* logprob_out_dev, float* stats_out_dev, float* entropy_out_dev, void* workspace_dev, size_t workspace_bytes, int32_t* status_dev,
                              void* stream) {
   if (!a_dev || !w_dev || rows <= 0 || C <= 0 || (C % 8) || V <= 0 || (V % 8) || !(tau >= 1e-6f && tau <= 1e6f)) return FV_ERR_INVALID_ARG;
-  if (!aligned_to(a_dev, 16) || !aligned_to(w_dev, 16) || !aligned_to(bias_dev, 2) || !workspace_dev || !aligned_to(workspace_dev, 256)) return FV_ERR_INVALID_ARG;
+  if (!aligned_to(a_dev, 16) || !aligned_to(w_dev, 16) || !aligned_to(bias_dev, 16) || !workspace_dev || !aligned_to(workspace_dev, 256)) return FV_ERR_INVALID_ARG;
   if ((ids_dev != nullptr) != (logprob_out_dev != nullptr) || !aligned_to(stats_out_dev, 8) || (!logprob_out_dev && !stats_out_dev && !entropy_out_dev)) return FV_ERR_INVALID_ARG;
-  if ((long long)((rows + 255) / 256) * ((V + 63) / 64) > INT_MAX) return FV_ERR_UNSUPPORTED;
+  if ((long long)((rows + 255) / 256) * ((V + 127) / 128) > INT_MAX) return FV_ERR_UNSUPPORTED;
   if (workspace_bytes < fv_linear_logprobs_workspace_bytes(rows, V)) return FV_ERR_CAPACITY;
+  if (C <= kFewK && few_rows_bytes(rows, V) > 0) {
+    const fv_status s = fv_gemm_bf16(a_dev, w_dev, bias_dev, rows, V, C, EPI_F32, workspace_dev, nullptr, nullptr, 0, rows, status_dev, nullptr, 0, stream);
+    if (s != FV_OK) return s;
+    return fv_token_logprobs(workspace_dev, 0, V, rows, V, tau, ids_dev, 0, logprob_out_dev, stats_out_dev, entropy_out_dev, nullptr, nullptr, status_dev, stream);
+  }
   if (linear_init() != cudaSuccess) return FV_ERR_CUDA;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   float4* part = static_cast<float4*>(workspace_dev);
-  float* xid = reinterpret_cast<float*>(static_cast<char*>(workspace_dev) + align_up((size_t)rows * column_parts(V) * sizeof(float4), 256));
-  const int bn = pick_width(rows, V, C, 74), parts = 2 * ((V + bn - 1) / bn);
+  float* xid = reinterpret_cast<float*>(static_cast<char*>(workspace_dev) + align_up((size_t)rows * column_parts(rows, V) * sizeof(float4), 256));
+  const int bn = tile_width(rows, V), parts = column_parts(rows, V);
   {
     LaunchScope scope(KC_GEMM, 1, 2.0 * rows * (double)V * C, 2.0 * ((double)rows * C + (double)V * C) + 16.0 * rows * parts, st);
     const LinearArgs p{rows, V, C, kLog2e * (1.f / tau), static_cast<const __nv_bfloat16*>(bias_dev), ids_dev, part, xid, status_dev};
-    const cudaError_t e = bn == 256 ? launch_width<256>(a_dev, w_dev, p, st) : bn == 128 ? launch_width<128>(a_dev, w_dev, p, st) : launch_width<64>(a_dev, w_dev, p, st);
+    const cudaError_t e = bn == 256 ? launch_width<256>(a_dev, w_dev, p, st) : launch_width<128>(a_dev, w_dev, p, st);
     if (e != cudaSuccess) return FV_ERR_CUDA;
   }
   const double bytes = 16.0 * rows * parts + 20.0 * rows;
   LaunchScope scope(KC_SELECT, 1, bytes, bytes, st);
   const FinishArgs f{part, xid, ids_dev, rows, V, parts, kLog2e * (1.f / tau), 1.f / tau, logprob_out_dev, reinterpret_cast<float2*>(stats_out_dev), entropy_out_dev, status_dev};
-  return launch_pdl(linear_finish_kernel, dim3((unsigned)((rows + 31) / 32)), dim3(32 * kFinishWarps), 0, st, f) == cudaSuccess ? FV_OK : FV_ERR_CUDA;
+  const cudaError_t e = parts < kManyParts ? launch_pdl(linear_finish_kernel<32>, dim3((unsigned)((rows + 31) / 32)), dim3(kFinishThreads), 0, st, f)
+                                           : launch_pdl(linear_finish_kernel<8>, dim3((unsigned)((rows + 7) / 8)), dim3(kFinishThreads), 0, st, f);
+  return e == cudaSuccess ? FV_OK : FV_ERR_CUDA;
 }
 
 }  // extern "C"

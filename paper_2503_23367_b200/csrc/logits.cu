@@ -4,9 +4,11 @@
 //     logprob(id) = d_id - L,     H = L - sum_j exp(d_j) d_j / s
 //     d logprob / dx_j = (1[j = id] - p_j) / tau,     dH / dx_j = -p_j (ln p_j + H) / tau
 //     loss = sum_k q_k (ln q_k - ln p_{id_k}),  q = softmax(t / tau),     d loss / dx_j = (p_j - sum_{k: id_k = j} q_k) / tau
-// Everything here moves a row through the chip once and does a handful of operations per logit, so DRAM bounds it.  A row (or, in a
-// thread-block cluster, a CTA's part of it) is copied to shared memory asynchronously and stays there: the maximum, the sums with
-// the maximum known, the alternatives and the gradient are passes over shared memory, and no pass rescales another's sums.
+// Everything here does a handful of operations per logit, so DRAM bounds it where there is work enough, and in the smallest calls the chain of
+// dependent steps.  Three forms, by what has to be known of a row before it can be left:
+//   statistics, alternatives, the loss alone: rows stream through the registers once (Stream, token_logprobs_kernel, distill_loss_kernel);
+//   the loss with its gradient: rows stay in shared memory between the sums and the gradient (Slice, distill_kernel);
+//   gradients from known statistics: a warp per 128 or 256 vectors of a row, no shared memory (Segment, *_grad_kernel).
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 

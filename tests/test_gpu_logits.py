@@ -141,6 +141,75 @@ def test_forward_matches_the_definition(rows, V, pad, shift, dtype):
     assert torch.equal(buf, before)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows,V", [(3, 900), (1300, 900), (5, 40007)])
+@pytest.mark.parametrize("tau", [1e-6, 0.01, 50.0, 1e6])
+def test_temperatures_far_from_one(rows, V, dtype, tau):
+    """Exponents of up to 2e7 (all but the largest vanish) and of almost 0 (everything is equally likely)."""
+    x, _ = rows_of(rows, V, dtype, 17)
+    ids = torch.randint(0, V, (rows,), device=DEV).to(torch.int32)
+    r, ref = check_forward(x, ids, tau, 3)
+    t_ids, t_logits = teacher_of(rows, V, 6, 4)
+    d = fv.fv_distill_topk(x, t_ids, t_logits, tau=tau, want_grad=True)
+    want = ref.loss(t_ids, t_logits)
+    near(d["loss"], want, LN + U * 400 * (want.abs() + 1))
+    want = ref.loss_grad(t_ids, t_logits, None)
+    # p and q carry the rounding of their exponents, u times up to 150 where they are not 0, twice for the two subtractions
+    near(d["dlogits"], want, (torch.finfo(dtype).eps / 2 if dtype != F32 else 0) * want.abs() + (LN + 600 * U) / tau)
+
+
+@pytest.mark.parametrize("dtype,V", [(F32, 393216), (BF16, 786432), (BF16, 786431)])
+def test_the_longest_rows(dtype, V):
+    x, _ = rows_of(2, V, dtype, 3)
+    ids = torch.tensor([V - 1, -1], dtype=torch.int32, device=DEV)
+    for n_alt in (3, 64):
+        check_forward(x, ids, 1.0, n_alt)
+    g = torch.tensor([0.5, -1.0], device=DEV)
+    check_token_grad(x, ids, g, g, 1.0)
+    check_distill(x, *teacher_of(2, V, 100, 5), g, 1.0)
+
+
+def test_many_rows_of_32_kb():
+    """Enough rows that a warp takes each, of a length that fewer rows give to a CTA."""
+    x, _ = rows_of(3600, 8190, F32, 19)
+    ids = torch.randint(0, 8190, (3600,), device=DEV).to(torch.int32)
+    for n_alt in (0, 8, 30):
+        check_forward(x, ids, 1.0, n_alt)
+
+
+def test_large_values_in_one_part_of_a_row():
+    """The alternatives lie side by side in one CTA's part of the row, and at its ends."""
+    for rows, V in ((1, 131072), (3, 262144), (1300, 4096)):
+        x, _ = rows_of(rows, V, F32, 23)
+        x[:, 1000:1100] += 20.0
+        x[:, -40:] += 30.0
+        x[:, :3] += 40.0
+        ids = torch.zeros(rows, dtype=torch.int32, device=DEV)
+        for n_alt in (10, 24, 64):
+            check_forward(x, ids, 1.0, n_alt)
+
+
+def test_refusals_of_the_binding():
+    x = torch.randn(4, 100, device=DEV); ids = torch.zeros(4, dtype=torch.int32, device=DEV)
+    f = fv.fv_token_logprobs(x, ids, want_entropy=True)
+    t_ids = torch.zeros(4, 3, dtype=torch.int32, device=DEV); t_logits = torch.zeros(4, 3, device=DEV)
+    bad = [lambda: fv.fv_token_logprobs(x[0]), lambda: fv.fv_token_logprobs(x.half()), lambda: fv.fv_token_logprobs(x.t()), lambda: fv.fv_token_logprobs(x, ids.long()),
+           lambda: fv.fv_token_logprobs(x, ids[:3]), lambda: fv.fv_token_logprobs(x, ids.cpu()), lambda: fv.fv_token_logprobs(x.cpu(), ids),
+           lambda: fv.fv_token_logprobs_grad(x, ids, f["stats"][:3], ids.float()), lambda: fv.fv_token_logprobs_grad(x, ids, f["stats"], ids),
+           lambda: fv.fv_token_logprobs_grad(x, ids, f["stats"], ids.float(), out=x.bfloat16()), lambda: fv.fv_token_logprobs_grad(x, ids, f["stats"], ids.float(), out=x[:3]),
+           lambda: fv.fv_distill_topk(x, t_ids, t_logits[:, :2]), lambda: fv.fv_distill_topk(x, t_ids.long(), t_logits), lambda: fv.fv_distill_topk(x, t_ids, t_logits.bfloat16()),
+           lambda: fv.fv_linear_logprobs(x, x, None), lambda: fv.fv_linear_logprobs(x.bfloat16(), x[:, :96].bfloat16(), None)]
+    for call in bad:
+        with pytest.raises(AssertionError):
+            call()
+    with pytest.raises(fv.FvError) as e:
+        fv.fv_token_logprobs(x, ids, n_alt=65)
+    assert e.value.code == 1
+    with pytest.raises(fv.FvError) as e:
+        fv.fv_token_logprobs(torch.zeros(1, 400000, device=DEV))
+    assert e.value.code == 4
+
+
 def test_each_output_alone_is_the_same():
     x, _ = rows_of(37, 5000, BF16, 3)
     ids = torch.randint(0, 5000, (37,), device=DEV).to(torch.int32)
@@ -409,6 +478,36 @@ def test_linear_logprobs_match_the_definition(rows, Cw, V, bias, tau):
     near(r["stats"][:, 1], ref.L, 2 * e + LN)
     near(r["logprob"], ref.logprob(ids), 2 * e + LN + 200 * U)
     near(r["entropy"], ref.H, 40 * e + 2 * LN + 200 * U * ref.H.abs())
+
+
+def test_linear_logprobs_with_forbidden_tokens():
+    """A bias of -inf forbids a token: p = 0, and where it forbids all, every statistic is -inf and the entropy 0."""
+    g = torch.Generator(device=DEV).manual_seed(3)
+    for rows in (7, 300):                # the few-row route and the tiles
+        a = torch.randn(rows, 128, device=DEV, generator=g).bfloat16()
+        w = (torch.randn(1024, 128, device=DEV, generator=g) * 0.2).bfloat16()
+        b = torch.where(torch.rand(1024, device=DEV, generator=g) < 0.7, -INF, 0.1).bfloat16()
+        ids = torch.randint(-1, 1024, (rows,), device=DEV, generator=g).to(torch.int32)
+        ref = Ref(a.double() @ w.double().t() + b.double(), 1.0)
+        r = fv.fv_linear_logprobs(a, w, b, ids, want_entropy=True)
+        near(r["stats"][:, 1], ref.L, 1e-5)
+        near(r["logprob"], ref.logprob(ids), 1e-5)
+        near(r["entropy"], ref.H, 1e-4)
+        r = fv.fv_linear_logprobs(a, w, torch.full_like(b, -INF), ids, want_entropy=True)
+        assert (r["stats"] == -INF).all() and (r["entropy"] == 0).all()
+        assert (r["logprob"] == torch.where(ids < 0, 0.0, -INF)).all()
+
+
+def test_linear_logprobs_ids_none_or_outside():
+    a = torch.randn(70, 64, device=DEV).bfloat16(); w = torch.randn(256, 64, device=DEV).bfloat16()
+    st = torch.zeros(1, dtype=torch.int32, device=DEV)
+    for rows in (3, 70):
+        ids = torch.zeros(rows, dtype=torch.int32, device=DEV)
+        ids[0], ids[1] = -1, 256
+        st.zero_()
+        r = fv.fv_linear_logprobs(a[:rows], w, None, ids, status=st)
+        assert int(st) == 40 and float(r["logprob"][0]) == 0 and torch.isnan(r["logprob"][1]) and torch.isfinite(r["logprob"][2:]).all()
+        assert set(fv.fv_linear_logprobs(a[:rows], w, None)) == {"stats"}
 
 
 # ------------------------------------------------------------------------------------------------ streams and graphs
