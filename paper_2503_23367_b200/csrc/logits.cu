@@ -229,7 +229,7 @@ struct RowsArgs {
 // the maximum passes it by 2^64.  The blocks come through a ring in shared memory in which every lane has its own slots: copies of
 // kAhead blocks are on their way while one is summed, which in registers would cost half of the warps.  Nothing of the row is kept; what holds
 // the alternatives is read again, from L2.
-constexpr int kStreamThreads = 128, kStreamWarps = 4, kBlock = 4, kAhead = 2;
+constexpr int kStreamThreads = 128, kStreamWarps = 4, kBlock = 4, kAhead = 1;
 constexpr int kRingBytes = (kAhead + 1) * kBlock * 32 * 16;   // of a warp
 constexpr int kMaxWarps = kMaxCluster * kStreamWarps;   // warps that share a row
 
@@ -454,10 +454,10 @@ template <typename T> __device__ __forceinline__ uint32_t reach_bits(const uint4
   return bits;
 }
 
-// The warp's elements that reach thr, at most most of them where there are many.  bm: [turns][32] maxima of the lanes' blocks.  A few blocks hold one: their vectors
+// The warp's elements that reach thr, at most `most` of them where there are many.  bm: [turns][32] maxima of the lanes' blocks.  A few blocks hold one: their vectors
 // are read again, spread over the warp.  Where they are too many (rows of mostly equal values, rows in order), the warp goes over all of its
 // vectors once more and keeps the largest `most` of what it has met whenever it runs out of room.
-template <typename T, int G> __device__ __forceinline__ void warp_select(const Stream<T, G>& st, const float* bm, float partial_max, float thr, int most, WarpAlt& wa, Found& f) {
+template <typename T, int G> __device__ __forceinline__ void warp_select(const Stream<T, G>& st, const T* bm, float partial_max, float thr, int most, WarpAlt& wa, Found& f) {
   constexpr int B = Stream<T, G>::B;
   const int lane = st.t & 31, turns = st.turns();
   const uint32_t below = (1u << lane) - 1;
@@ -475,7 +475,7 @@ template <typename T, int G> __device__ __forceinline__ void warp_select(const S
   for (int k0 = 0; k0 < turns; k0 += 4) {
     float b[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) b[i] = k0 + i < turns ? bm[(k0 + i) * 32 + lane] : -INFINITY;
+    for (int i = 0; i < 4; ++i) b[i] = k0 + i < turns ? float(bm[(k0 + i) * 32 + lane]) : -INFINITY;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const bool hit = b[i] >= thr;
@@ -535,7 +535,7 @@ template <typename T, int G> __device__ __forceinline__ void warp_select(const S
   };
   if (__any_sync(0xFFFFFFFFu, mine)) over(u, mine ? reach_bits<T>(u, thr) : 0, st.part * Elem<T>::E - st.off);
   for (int q = 0; q < turns * B; ++q) {
-    if (!__any_sync(0xFFFFFFFFu, bm[q / B * 32 + lane] >= thr)) continue;
+    if (!__any_sync(0xFFFFFFFFu, float(bm[q / B * 32 + lane]) >= thr)) continue;
     const int j = st.t + q * G;
     uint4 x{};
     if (j < st.nw) x = st.load(j);
@@ -594,10 +594,10 @@ __global__ void __launch_bounds__(kStreamThreads, 8) token_logprobs_kernel(const
   pdl_wait();
   if (G == 32 && row >= p.r.rows) return;
   // shared memory: per warp a ring, whose place the scratch of the alternatives takes later, and its block maxima; what warps share and their lists of alternatives
-  const size_t per_warp = kRingBytes + (ALT ? (size_t)p.turns * 128 : 0);
+  const size_t per_warp = kRingBytes + (ALT ? (size_t)p.turns * 32 * sizeof(T) : 0);
   uint4* ring = reinterpret_cast<uint4*>(reinterpret_cast<char*>(smem) + warp * per_warp);
   WarpAlt& wa = *reinterpret_cast<WarpAlt*>(ring);
-  float* bm = reinterpret_cast<float*>(reinterpret_cast<char*>(ring) + kRingBytes);
+  T* bm = reinterpret_cast<T*>(reinterpret_cast<char*>(ring) + kRingBytes);   // (a maximum of Ts is a T)
   Shared& sh = *reinterpret_cast<Shared*>(reinterpret_cast<char*>(smem) + W * per_warp);
   RowAlt& ra = *reinterpret_cast<RowAlt*>(&sh + 1);
   unsigned long long* lists = reinterpret_cast<unsigned long long*>(&ra + 1);   // [warps][n_alt]
@@ -610,13 +610,12 @@ __global__ void __launch_bounds__(kStreamThreads, 8) token_logprobs_kernel(const
   Online<T, ENT> on(c);
   float partial_max = -INFINITY;
   if (ALT)                             // the thread's last block, which may be short, and those that it does not have
-    for (int k = (st.t < st.nw ? (st.nw - st.t + G - 1) / G : 0) / Stream<T, G>::B; k < st.turns(); ++k) bm[k * 32 + lane] = -INFINITY;
+    for (int k = (st.t < st.nw ? (st.nw - st.t + G - 1) / G : 0) / Stream<T, G>::B; k < st.turns(); ++k) Elem<T>::store(bm + k * 32 + lane, -INFINITY);
   st.each(ring, [&](const uint4* u, auto n, int k) {
     const float b = on.template add<decltype(n)::value>(u);
     if (ALT) {
       if (k < 0) partial_max = b;
-      else if (decltype(n)::value > 1) bm[k * 32 + lane] = b;
-      else bm[k * 32 + lane] = fmaxf(bm[k * 32 + lane], b);
+      else Elem<T>::store(bm + k * 32 + lane, decltype(n)::value > 1 ? b : fmaxf(float(bm[k * 32 + lane]), b));
     }
   });
   float xid = 0.f;
@@ -1258,7 +1257,7 @@ template <typename K, typename A> cudaError_t go_rows(K kernel, int threads, A& 
 template <typename T, int G> cudaError_t go_token(TokenArgs& a, const Shape& s, cudaStream_t st) {
   a.turns = (s.per_max + Stream<T, G>::B * G - 1) / (Stream<T, G>::B * G);
   const size_t rows = kStreamWarps * (size_t)kRingBytes + (G == 32 ? 0 : sizeof(Shared));
-  const size_t with = rows + kStreamWarps * (size_t)a.turns * 128 + (G == 32 ? 0 : sizeof(RowAlt) + ((size_t)a.n_alt * kStreamWarps * 8 << s.lg));
+  const size_t with = rows + kStreamWarps * (size_t)a.turns * 32 * sizeof(T) + (G == 32 ? 0 : sizeof(RowAlt) + ((size_t)a.n_alt * kStreamWarps * 8 << s.lg));
   if (a.n_alt > 0)
     return a.entropy ? go_rows(token_logprobs_kernel<T, G, true, true>, kStreamThreads, a, s, with, st) : go_rows(token_logprobs_kernel<T, G, false, true>, kStreamThreads, a, s, with, st);
   return a.entropy ? go_rows(token_logprobs_kernel<T, G, true, false>, kStreamThreads, a, s, rows, st) : go_rows(token_logprobs_kernel<T, G, false, false>, kStreamThreads, a, s, rows, st);
