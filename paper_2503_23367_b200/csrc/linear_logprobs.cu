@@ -66,6 +66,8 @@ template <int N> __device__ __forceinline__ float pick(const float* acc, int i) 
   }
 }
 
+// Bound by the product: 8192 x 2048 -> 4096 97 us, 1.42 PFLOP/s (the plain bf16 GEMM of the shape 92); a round of tiles ends with one epilogue that nothing
+// covers (1.6 us), small calls are the fixed cost of a pair kernel (169 x 1024 -> 4096 9 us with the second launch).
 template <int BN>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 linear_logprobs_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const LinearArgs p) {

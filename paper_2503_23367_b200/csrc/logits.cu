@@ -65,7 +65,6 @@ template <> struct Elem<float> {
   }
   static __device__ __forceinline__ float load(const float* p) { return dep_load(p); }
   static __device__ __forceinline__ void store(float* p, float v) { *p = v; }
-  static __device__ __forceinline__ float round(float v) { return v; }
   // running maximum of a thread
   struct Max {
     float m = -INFINITY;
@@ -583,6 +582,10 @@ template <typename T, bool ENT> __device__ __forceinline__ void tell_row(const T
   p.logprob[row] = lp;
 }
 
+// One read of the rows; per logit 4.6 instructions (bf16; 2.5 fp32) with one exponential, 1.5 more with the entropy, and per row some 400 for a warp's own
+// bookkeeping, 1000 more with alternatives.  So long rows are bound by DRAM (4800 x 32768 fp32 93 us, 6.8 TB/s with what L2 held) or, bf16 with entropy and alternatives, by instructions (3001 x 50021
+// 74 us, issue 69 %); many short rows by how many are on their way beside the 7 000 clocks of bookkeeping behind each (8192 x 4096 fp32, 8 alternatives, 29 us, 4.6 TB/s); few rows by
+// the chain of steps (two of 4096 with 5 alternatives 4.6 us, four of 131072 with 20 on clusters of eight 11.5).
 template <typename T, int G, bool ENT, bool ALT>
 __global__ void __launch_bounds__(kStreamThreads, 8) token_logprobs_kernel(const TokenArgs p) {
   constexpr int W = kStreamWarps;
@@ -875,6 +878,8 @@ template <typename T, int G> __device__ __forceinline__ Part thread_part(const S
 
 struct alignas(16) DistillScratch { Part part[64]; TeacherRow tr; };
 
+// One read and one write of the rows, two exponentials per logit: 4096 x 131072 bf16 380 us, 5.7 TB/s with the exponentials' unit 67 % busy; 8192 x 4096 fp32 45 us, 5.9 TB/s.  The
+// row could be read a second time from L2 instead of being kept; that is 1.5 times L2's traffic where L2 is the faster by less.
 template <typename T, int G>
 __global__ void __launch_bounds__(G + 32, G == 64 ? 10 : 768 / G) distill_kernel(const DistillArgs p) {
   constexpr int W = G / 32, E = Elem<T>::E, P = Teacher::P;
@@ -951,6 +956,7 @@ __global__ void __launch_bounds__(G + 32, G == 64 ? 10 : 768 / G) distill_kernel
   }
 }
 
+// One read of the rows, then the teacher's entries (two dependent reads, some 150 instructions) by a warp: 1025 x 32768 bf16 15.6 us, 4.3 TB/s of one round of CTAs.
 // The loss alone: nothing of the row is needed again but the logits of the teacher's tokens.
 template <typename T, int G>
 __global__ void __launch_bounds__(kStreamThreads, 8) distill_loss_kernel(const DistillArgs p) {
@@ -1008,7 +1014,7 @@ struct GradArgs {
   void* dx; long long ld_dx;
   int32_t* status;
 };
-constexpr int kGradWarps = 4, UB = 4, UF = 4, UD = 8;
+constexpr int kGradWarps = 4, kGradVectors = 4, kDistillGradVectors = 8;   // warps of a CTA; vectors of a lane
 
 // The part of a row that a warp takes: where its vectors lie, what they hold, how they are written.
 template <typename T, int U> struct Segment {
@@ -1068,6 +1074,8 @@ struct LogP {
   __device__ __forceinline__ uint64_t operator()(uint64_t x) const { return fma2(add2(x, neg_m), c, neg_L); }
 };
 
+// Bound by DRAM: 8192 x 4096 fp32 with entropy 42 us, 6.4 TB/s; 2003 x 50021 bf16 60 us, 6.7 TB/s (what stays in L2 at the end included).  U of 2 / 4 / 8: fp32 56 / 48 / 51 us
+// before loads and stores were marked to leave the caches first, which is worth 6 us more.
 template <typename T, int U, bool ENT>
 __global__ void __launch_bounds__(32 * kGradWarps) token_logprobs_grad_kernel(const GradArgs p) {
   constexpr int E = Elem<T>::E;
@@ -1119,6 +1127,7 @@ __global__ void __launch_bounds__(32 * kGradWarps) token_logprobs_grad_kernel(co
   }
 }
 
+// As above, and every warp weighs the teacher's entries itself (some 200 instructions beside 600 for its logits: U 8).  2048 x 16384 fp32, K 32: 45 us, 6 TB/s.
 template <typename T, int U>
 __global__ void __launch_bounds__(32 * kGradWarps) distill_grad_kernel(const GradArgs p) {
   constexpr int E = Elem<T>::E;
@@ -1333,8 +1342,8 @@ fv_status fv_token_logprobs_grad(const void* logits_dev, int32_t dtype, int64_t 
   GradArgs a{logits_dev, ld, rows, V, 0, 1.f / tau, reinterpret_cast<const float2*>(stats_dev), entropy_dev, ids_dev, g_logprob_dev, g_entropy_dev,
              nullptr, nullptr, 0, dlogits_out_dev, ld_out, status_dev};
   using B = __nv_bfloat16;
-  if (dtype) return cu(g_entropy_dev ? launch_grad<B, UB>(token_logprobs_grad_kernel<B, UB, true>, a, st) : launch_grad<B, UB>(token_logprobs_grad_kernel<B, UB, false>, a, st));
-  return cu(g_entropy_dev ? launch_grad<float, UF>(token_logprobs_grad_kernel<float, UF, true>, a, st) : launch_grad<float, UF>(token_logprobs_grad_kernel<float, UF, false>, a, st));
+  if (dtype) return cu(g_entropy_dev ? launch_grad<B, kGradVectors>(token_logprobs_grad_kernel<B, kGradVectors, true>, a, st) : launch_grad<B, kGradVectors>(token_logprobs_grad_kernel<B, kGradVectors, false>, a, st));
+  return cu(g_entropy_dev ? launch_grad<float, kGradVectors>(token_logprobs_grad_kernel<float, kGradVectors, true>, a, st) : launch_grad<float, kGradVectors>(token_logprobs_grad_kernel<float, kGradVectors, false>, a, st));
 }
 
 fv_status fv_distill_topk(const void* logits_dev, int32_t dtype, int64_t ld, int32_t rows, int32_t V, float tau, const int32_t* teacher_ids_dev,
@@ -1365,7 +1374,8 @@ fv_status fv_distill_topk_grad(const void* logits_dev, int32_t dtype, int64_t ld
   LaunchScope scope(KC_SELECT, 1, bytes, bytes, st);
   GradArgs a{logits_dev, ld, rows, V, 0, 1.f / tau, reinterpret_cast<const float2*>(stats_dev), nullptr, nullptr, g_loss_dev, nullptr,
              teacher_ids_dev, teacher_logits_dev, K, dlogits_out_dev, ld_out, status_dev};
-  return cu(dtype ? launch_grad<__nv_bfloat16, UD>(distill_grad_kernel<__nv_bfloat16, UD>, a, st) : launch_grad<float, UD>(distill_grad_kernel<float, UD>, a, st));
+  return cu(dtype ? launch_grad<__nv_bfloat16, kDistillGradVectors>(distill_grad_kernel<__nv_bfloat16, kDistillGradVectors>, a, st)
+                  : launch_grad<float, kDistillGradVectors>(distill_grad_kernel<float, kDistillGradVectors>, a, st));
 }
 
 }  // extern "C"
