@@ -262,7 +262,7 @@ template <typename T, int G> struct Stream {
       f[e / 2] = pack2(i0 + e >= 0 && i0 + e < V ? x[e] : -INFINITY, i0 + e + 1 >= 0 && i0 + e + 1 < V ? x[e + 1] : -INFINITY);
     return Elem<T>::pack(f);
   }
-  // f(vectors, how many, block) for the thread's blocks of up to B vectors, the partial one last and alone (block -1).  ring: the warp's.
+  // f(vectors, how many, block) for the thread's blocks of up to B vectors (32 apart in the ring), the partial one last and alone (block -1).  ring: the warp's.
   template <typename F> __device__ __forceinline__ void each(uint4* ring, F f) const {
     const uint32_t slot = smem_u32(ring + (t & 31));
     const char* g = base + (size_t)t * 16;
@@ -283,10 +283,7 @@ template <typename T, int G> struct Stream {
       asm volatile("cp.async.wait_group %0;" ::"n"(kAhead) : "memory");
       const uint4* mine = ring + s * B * 32 + (t & 31);
       if (left > (B - 1) * G) {
-        uint4 a[B];
-#pragma unroll
-        for (int i = 0; i < B; ++i) a[i] = mine[i * 32];
-        f(a, std::integral_constant<int, B>(), k);
+        f(mine, std::integral_constant<int, B>(), k);
       } else {
         for (int i = 0; left > i * G; ++i) f(mine + i * 32, std::integral_constant<int, 1>(), k);
       }
@@ -304,10 +301,10 @@ template <typename T, bool ENT> struct Online {
   float c, m = -INFINITY, R = 0.f, limit = -INFINITY;   // limit: largest maximum that the reference bears
   Sums<T, ENT> sums;
   __device__ __forceinline__ explicit Online(float c_) : c(c_) {}
-  template <int N> __device__ __forceinline__ float add(const uint4* u) {   // the vectors' maximum
+  template <int N> __device__ __forceinline__ float add(const uint4* u) {   // u: N vectors of the ring, 32 apart; their maximum
     typename Elem<T>::Max mx;
 #pragma unroll
-    for (int i = 0; i < N; ++i) mx.add(u[i]);
+    for (int i = 0; i < N; ++i) mx.add(u[i * 32]);
     const float bm = mx.value();
     m = fmaxf(m, bm);
     if (bm > limit) {
@@ -326,7 +323,7 @@ template <typename T, bool ENT> struct Online {
     }
     const Expo<true> ex(R, c);
 #pragma unroll
-    for (int i = 0; i < N; ++i) sums.add(u[i], ex);
+    for (int i = 0; i < N; ++i) sums.add(u[i * 32], ex);
     return bm;
   }
   __device__ __forceinline__ Part part() const { return part_of(m, sums, delta(safe_max(m), c, R)); }
@@ -337,7 +334,7 @@ template <typename T, int G, bool ENT> __device__ __forceinline__ Part far_part(
   const Expo<false> ex(m, c);
   st.each(ring, [&](const uint4* u, auto n, int) {
 #pragma unroll
-    for (int i = 0; i < decltype(n)::value; ++i) sums.add(u[i], ex);
+    for (int i = 0; i < decltype(n)::value; ++i) sums.add(u[i * 32], ex);
   });
   return part_of(m, sums, 0.f);
 }
@@ -355,32 +352,37 @@ static_assert(sizeof(WarpAlt) <= kRingBytes, "takes the ring's place");
 struct alignas(16) RowAlt {        // of a row that warps share (in every CTA of a cluster)
   float own[kThreadGroups], all[kThreadGroups];   // maxima of groups of threads, of this CTA and of the cluster
   float bound[kMaxCluster];        // what the cluster's CTAs found on their own
-  float nth;
+  float least[kStreamWarps];
   int count[kMaxWarps];            // of the warps' lists, which lie behind this: [warps][n_alt], in the cluster's first CTA
 };
 
-__device__ __forceinline__ int rank_among(float my, int i, const float* gm, int n) {   // how many of gm are larger, or equal and in front of i
-  int rank = 0;
+__device__ __forceinline__ int larger_than(float my, const float* gm, int n) {   // how many of gm are
+  int count = 0;
 #pragma unroll 8
   for (int j = 0; j < n; j += 4) {
     const float4 v = *reinterpret_cast<const float4*>(gm + j);
-    rank += (v.x > my || (v.x == my && j < i)) + (v.y > my || (v.y == my && j + 1 < i)) + (v.z > my || (v.z == my && j + 2 < i)) + (v.w > my || (v.w == my && j + 3 < i));
+    count += (v.x > my) + (v.y > my) + (v.z > my) + (v.w > my);
   }
-  return rank;
+  return count;
 }
-// The n-th largest of the maxima of 32 groups of threads: at least n of the elements that they went over reach it, about n (1 + n / 40) where large
-// values are spread over them.  Every warp for itself.
+__device__ __forceinline__ float warp_min(float v) {
+  float r;
+  asm volatile("redux.sync.min.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
+  return r;
+}
+// The n-th largest of the maxima of 32 groups of threads, which is the smallest that fewer than n exceed: at least n of the elements that the groups went over
+// reach it, about n (1 + n / 40) where large values are spread over them.  Every warp for itself.
 __device__ __forceinline__ float nth_of_32(const float* gm, int n, int lane) {
   const float my = gm[lane];
-  const uint32_t who = __ballot_sync(0xFFFFFFFFu, rank_among(my, lane, gm, 32) == n - 1);
-  return __shfl_sync(0xFFFFFFFFu, my, __ffs(who) - 1);
+  return warp_min(larger_than(my, gm, 32) < n ? my : INFINITY);
 }
-// The same of 128 groups (1.2 n elements at n 64), by the CTA.
-__device__ __forceinline__ float nth_of_128(const float* gm, float* out, int n) {
+// The same of 128 groups (1.2 n elements at n 64), by the CTA.  least: [4] of the CTA's own.
+__device__ __forceinline__ float nth_of_128(const float* gm, float* least, int n) {
   const float my = gm[threadIdx.x];
-  if (rank_among(my, threadIdx.x, gm, kThreadGroups) == n - 1) *out = my;
+  const float w = warp_min(larger_than(my, gm, kThreadGroups) < n ? my : INFINITY);
+  if ((threadIdx.x & 31) == 0) least[threadIdx.x >> 5] = w;
   __syncthreads();
-  const float r = *out;
+  const float r = fminf(fminf(least[0], least[1]), fminf(least[2], least[3]));
   __syncthreads();
   return r;
 }
@@ -479,6 +481,7 @@ template <typename T, int G> __device__ __forceinline__ void warp_select(const S
     for (int i = 0; i < 4; ++i) {
       const bool hit = b[i] >= thr;
       const uint32_t who = __ballot_sync(0xFFFFFFFFu, hit);
+      if (!who) continue;
       const int at = h + __popc(who & below);
       if (hit && at < kMaxCand) wa.hit[at] = (uint16_t)((k0 + i) * 32 + lane);
       h += __popc(who);
@@ -494,6 +497,7 @@ template <typename T, int G> __device__ __forceinline__ void warp_select(const S
     for (int i = 0; i < 4; ++i) {
       const int q = q0 + 32 * i + lane;
       j[i] = st.nw;
+      if (q0 + 32 * i >= B * h) continue;
       if (q < B * h) {
         const int code = wa.hit[q / B];
         j[i] = t0 + (code & 31) + ((code >> 5) * B + q % B) * G;
@@ -502,7 +506,7 @@ template <typename T, int G> __device__ __forceinline__ void warp_select(const S
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-      if (fits) fits = f.add<T>(v[i], j[i] < st.nw ? reach_bits<T>(v[i], thr) : 0, st.index_of(j[i]));
+      if (fits && q0 + 32 * i < B * h) fits = f.add<T>(v[i], j[i] < st.nw ? reach_bits<T>(v[i], thr) : 0, st.index_of(j[i]));
   }
   if (fits) {
     __syncwarp();
@@ -659,7 +663,7 @@ __global__ void __launch_bounds__(kStreamThreads, 8) token_logprobs_kernel(const
       const float g = lane_group_max(on.m, per);
       if (lane % (32 / per) == 0) ra.own[warp * per + lane / (32 / per)] = g;
       __syncthreads();
-      float thr = few ? nth_of_32(ra.own, p.n_alt, lane) : nth_of_128(ra.own, &ra.nth, p.n_alt);
+      float thr = few ? nth_of_32(ra.own, p.n_alt, lane) : nth_of_128(ra.own, ra.least, p.n_alt);
       if (parts > 1) {
         const int gw = per >> p.r.lg;                          // groups of a warp where the cluster has 32 or 128 (at least one: 8 CTAs have 32 warps)
         const float h = lane_group_max(on.m, gw);
@@ -670,7 +674,7 @@ __global__ void __launch_bounds__(kStreamThreads, 8) token_logprobs_kernel(const
         __syncwarp();
         cluster_sync_all();
         for (int i = 0; i < parts; ++i) thr = fmaxf(thr, ra.bound[i]);
-        thr = fmaxf(thr, few ? nth_of_32(ra.all, p.n_alt, lane) : nth_of_128(ra.all, &ra.nth, p.n_alt));
+        thr = fmaxf(thr, few ? nth_of_32(ra.all, p.n_alt, lane) : nth_of_128(ra.all, ra.least, p.n_alt));
       }
       thr = fmaxf(thr, Elem<T>::kLowest);                      // -inf is no alternative
       Found f;
