@@ -7,6 +7,7 @@ not been built.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 from typing import List, Optional, Sequence
 
@@ -486,6 +487,11 @@ def fv_distill_topk_grad(logits: torch.Tensor, teacher_ids: torch.Tensor, teache
     return out
 
 
+@functools.lru_cache(maxsize=256)
+def _linear_workspace_bytes(rows: int, V: int) -> int:
+    return lib().fv_linear_logprobs_workspace_bytes(rows, V)
+
+
 def fv_linear_logprobs(a: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Tensor], ids: Optional[torch.Tensor] = None, tau: float = 1.0,
                        want_entropy: bool = False, status: Optional[torch.Tensor] = None) -> dict:
     """As fv_token_logprobs on the rows a [rows, C] * w [V, C]^T + bias [V] (all bf16), whose logits are not kept."""
@@ -494,7 +500,7 @@ def fv_linear_logprobs(a: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Te
     dev, bf = a.get_device(), torch.bfloat16
     assert dev == torch._C._cuda_getDevice(), "the rows are on the current CUDA device"
     ap, wp, bp, idp = _arg(a, bf, (rows, Cw), dev), _arg(w, bf, (V, Cw), dev), _arg(bias, bf, (V,), dev), _arg(ids, _I32, (rows,), dev)
-    ws_bytes = lib().fv_linear_logprobs_workspace_bytes(rows, V)
+    ws_bytes = _linear_workspace_bytes(rows, V)
     ws = _new(ws_bytes + 256, a, torch.uint8)
     stats = _new2(rows, 2, a)
     r = {"stats": stats}

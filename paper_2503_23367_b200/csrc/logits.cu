@@ -171,11 +171,6 @@ template <typename T, int G> struct Slice {
     }
     for (; left > 0; left -= G, q += G) f(*q);
   }
-  __device__ __forceinline__ float element(int i) const {   // logit i of the row, which lies in this part
-    const int e = i + off - v0 * E;
-    if constexpr (sizeof(T) == 4) return reinterpret_cast<const float*>(s)[e];
-    else return __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(s)[e]);
-  }
 };
 
 // s = sum e and t = sum e d over vectors of logits.
@@ -587,9 +582,9 @@ template <typename T, bool ENT> __device__ __forceinline__ void tell_row(const T
 }
 
 // One read of the rows; per logit 4.6 instructions (bf16; 2.5 fp32) with one exponential, 1.5 more with the entropy, and per row some 400 for a warp's own
-// bookkeeping, 1000 more with alternatives.  So long rows are bound by DRAM (4800 x 32768 fp32 93 us, 6.8 TB/s with what L2 held) or, bf16 with entropy and alternatives, by instructions (3001 x 50021
-// 74 us, issue 69 %); many short rows by how many are on their way beside the 7 000 clocks of bookkeeping behind each (8192 x 4096 fp32, 8 alternatives, 29 us, 4.6 TB/s); few rows by
-// the chain of steps (two of 4096 with 5 alternatives 4.6 us, four of 131072 with 20 on clusters of eight 11.5).
+// bookkeeping, 700 more with alternatives.  So long rows are bound by DRAM (4800 x 32768 fp32 93 us, 6.8 TB/s with what L2 held) or, bf16 with entropy and alternatives, by
+// instructions (3001 x 50021, 20 alternatives, 70 us, issue 70 %); many short rows by how many are on their way beside the 6000 clocks of bookkeeping behind each (8192 x 4096
+// fp32, 8 alternatives, 27 us, 4.9 TB/s); few rows by the chain of steps (two of 4096 with 5 alternatives 4.2 us, four of 131072 with 20 on clusters of eight 6.9).
 template <typename T, int G, bool ENT, bool ALT>
 __global__ void __launch_bounds__(kStreamThreads, 8) token_logprobs_kernel(const TokenArgs p) {
   constexpr int W = kStreamWarps;
@@ -691,23 +686,35 @@ __global__ void __launch_bounds__(kStreamThreads, 8) token_logprobs_kernel(const
     if (!near) share_parts<ENT>(sh, warp_union<ENT>(far_part<T, G, ENT>(st, ring, m, c), c), 1, parts, rank, warp, lane);
     if (rank != 0 || (!ALT && warp != 0)) return;
     const Stat stat = stat_of_parts<ENT>(sh.part[near ? 0 : 1], warps, c, lane);
-    if constexpr (ALT) {               // every key's place is how many are larger
+    if constexpr (ALT) {               // the lists one behind the other, in a ring's place; then every key's place is how many are larger
       const int per = kStreamThreads / warps, l = threadIdx.x / per;   // threads of a list; this thread's
-      const int have = lane < warps ? ra.count[lane] : 0, total = __reduce_add_sync(0xFFFFFFFFu, have);
-      const int mine_n = __shfl_sync(0xFFFFFFFFu, have, l);
-      for (int i0 = 0; __any_sync(0xFFFFFFFFu, i0 + (int)threadIdx.x % per < mine_n); i0 += per) {
-        const int i = i0 + threadIdx.x % per;
-        const unsigned long long key = i < mine_n ? lists[(size_t)l * p.n_alt + i] : ~0ull;
-        int place = 0;
-        for (uint32_t left = __ballot_sync(0xFFFFFFFFu, have > 0); left; left &= left - 1) {
-          const int o = __ffs(left) - 1, n = __shfl_sync(0xFFFFFFFFu, have, o);
-          const unsigned long long* k = lists + (size_t)o * p.n_alt;
-#pragma unroll 8
-          for (int j = 0; j < n; ++j) place += k[j] > key;
-        }
-        if (i < mine_n && place < p.n_alt) tell_alt<ENT>(p, row, stat, place, key);
+      const int have = lane < warps ? ra.count[lane] : 0;
+      int upto = have;
+#pragma unroll
+      for (int o = 1; o < 32; o *= 2) {
+        const int v = __shfl_up_sync(0xFFFFFFFFu, upto, o);
+        if (lane >= o) upto += v;
       }
-      if ((int)threadIdx.x >= total && (int)threadIdx.x < p.n_alt) tell_alt<ENT>(p, row, stat, threadIdx.x, 0ull);
+      const int total = __shfl_sync(0xFFFFFFFFu, upto, 31), from = __shfl_sync(0xFFFFFFFFu, upto - have, l), n = __shfl_sync(0xFFFFFFFFu, have, l);
+      unsigned long long* all = reinterpret_cast<unsigned long long*>(smem);
+      static_assert((size_t)kMaxWarps * kMaxAlt * 8 + 16 <= W * ((size_t)kRingBytes + 32 * sizeof(T)), "32 lists of 64 keys and one more fit the rings and block maxima");
+      for (int i = threadIdx.x % per; i < n; i += per) all[from + i] = lists[(size_t)l * p.n_alt + i];
+      if (threadIdx.x == 0) all[total] = 0;                      // (keys are read in pairs)
+      __syncthreads();
+      for (int i = threadIdx.x; i < max(total, p.n_alt); i += kStreamThreads) {
+        unsigned long long key = 0;
+        int place = i;
+        if (i < total) {
+          key = all[i];
+          place = 0;
+#pragma unroll 4
+          for (int j = 0; j < total; j += 2) {
+            const ulonglong2 k = *reinterpret_cast<const ulonglong2*>(all + j);
+            place += (k.x > key) + (k.y > key);
+          }
+        }
+        if (place < p.n_alt) tell_alt<ENT>(p, row, stat, place, key);
+      }
     }
     if (scribe) tell_row<T, ENT>(p, row, stat, id, xid);
   }
