@@ -581,9 +581,9 @@ template <typename T, bool ENT> __device__ __forceinline__ void tell_row(const T
   p.logprob[row] = lp;
 }
 
-// One read of the rows; per logit 4.6 instructions (bf16; 2.5 fp32) with one exponential, 1.5 more with the entropy, and per row some 400 for a warp's own
-// bookkeeping, 700 more with alternatives.  So long rows are bound by DRAM (4800 x 32768 fp32 93 us, 6.8 TB/s with what L2 held) or, bf16 with entropy and alternatives, by
-// instructions (3001 x 50021, 20 alternatives, 70 us, issue 70 %); many short rows by how many are on their way beside the 6000 clocks of bookkeeping behind each (8192 x 4096
+// One read of the rows.  Counted per 32 logits of rows of 50021: 5.9 warp instructions (bf16; fp32 6.4) with one exponential per logit, 1.6 more with the entropy; and per
+// row, with alternatives, 740 more for a warp's (4096, 8 of them) or 4500 for four warps' (50021, 20 of them).  So long rows are bound by DRAM (4800 x 32768 fp32 93 us, 6.8 TB/s with what L2 held) or, bf16 with entropy and alternatives, by
+// instructions (3001 x 50021, 20 alternatives, 69 us, issue 68 %); many short rows by how many are on their way beside the 6700 clocks behind each one's last logit (8192 x 4096
 // fp32, 8 alternatives, 27 us, 4.9 TB/s); few rows by the chain of steps (two of 4096 with 5 alternatives 4.2 us, four of 131072 with 20 on clusters of eight 6.9).
 template <typename T, int G, bool ENT, bool ALT>
 __global__ void __launch_bounds__(kStreamThreads, 8) token_logprobs_kernel(const TokenArgs p) {
