@@ -308,8 +308,8 @@ template <int R> __global__ void __launch_bounds__(kFinishThreads) linear_finish
   p.logprob[row] = lp;
 }
 
-// Tile width: the cheaper by rounds, one of 128 columns costing 0.62 of one of 256 (us, 256 / 128 wide: 400 rows, C 2048, V 4096 17.6 / 13.2; 820 18.7 / 22.0; 5000, C 256,
-// V 1000 15.1 / 13.3; 8192, C 2048, V 4096 93 / 113; tiles of 64 columns were never faster).
+// Tile width: the cheaper by rounds, one of 128 columns costing 0.62 of one of 256 (us, 256 / 128 wide: 400 rows, C 2048, V 4096 17.6 / 12.8; 820 18.6 / 20.6; 5000, C 256,
+// V 1000 15.0 / 12.9; 8192, C 2048, V 4096 95 / 115; tiles of 64 columns were never faster).
 int tile_width(int M, int N) {
   const auto rounds = [&](int bn) { return (((long)(M + 2 * BM - 1) / (2 * BM)) * ((N + bn - 1) / bn) + 73) / 74; };
   return 0.62 * rounds(128) < rounds(256) ? 128 : 256;
@@ -335,7 +335,7 @@ template <int BN> cudaError_t launch_width(const void* a, const void* w, const L
 }
 
 // Few rows: the product with K split over a cluster (fv_gemm_bf16; its slices are at most 512 of K for these sizes, so its sums are as exact) and the rows read back from
-// L2, which is sooner done than 256-row tiles (one row, C 1024, V 4096: 10.8 -> 6 us).
+// L2, which is sooner done than 256-row tiles (one row, C 1024, V 4096: 10.8 -> 5.5 us).
 constexpr int kFewRows = 48, kFewColumns = 9472, kFewK = 2048;
 size_t few_rows_bytes(int rows, int V) { return rows <= kFewRows && V <= kFewColumns ? (size_t)rows * V * 4 : 0; }
 
