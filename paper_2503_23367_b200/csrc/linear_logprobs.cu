@@ -229,7 +229,7 @@ linear_logprobs_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
         struct { uint64_t s[2], t[2]; } sums;
         float dl = 0.f;
         if (is_near(m0, p.c)) {
-          const float R = whole_ref(m0, p.c);
+          const float R = reference(m0, p.c);
           sum(Expo<true>(R, p.c));
           dl = delta(m0, p.c, R);
         } else {

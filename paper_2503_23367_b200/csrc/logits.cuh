@@ -63,13 +63,14 @@ __device__ __forceinline__ void put_status(int32_t* status, int code) {
 }
 
 // ---- exponents ---------------------------------------------------------------------------------------------------------------
-// e = 2^d, d = (x - m) c, c = log2(e) / tau.  Near 0 (|m c| < 2^21) d is taken as x c - R in one operation, R the whole number next to m c (or to that of an
-// earlier maximum): R is exact, so all of a row's exponents are off by the one number m c - R, by which the sums are put right (delta).  That saves
-// half an instruction per logit.  Far from 0, where x c has no fraction left (masks of -1e9, of the type's lowest value), the difference is taken first.
+// e = 2^d, d = (x - m) c, c = log2(e) / tau.  Near 0 (|m c| < 2^21) d is taken as x c - R in one operation, rounded once, R = m c in fp32 (or that of an earlier maximum): all of a row's
+// exponents are off by the one number m c - R, by which the sums are put right (delta).  That saves half an instruction per logit.  For the maximum that R was taken from, delta is the
+// rounding of m c alone: the largest logit then adds 1 to s and next to nothing to t, and an entropy of almost 0 keeps its digits.  (With the whole number next to m c, t held up to half of s, and the
+// difference of the two was off by 2^-25.)  Far from 0, where x c has no fraction left (masks of -1e9, of the type's lowest value), the difference is taken first.
 constexpr float kFar = 2097152.f;      // 2^21
 __device__ __forceinline__ float safe_max(float m) { return m == -INFINITY ? 0.f : m; }
 __device__ __forceinline__ bool is_near(float m, float c) { return fabsf(m * c) < kFar; }
-__device__ __forceinline__ float whole_ref(float m, float c) { return fmaxf(rintf(m * c), -2.f * kFar); }   // a thread far below the row's maximum adds nothing
+__device__ __forceinline__ float reference(float m, float c) { return fmaxf(m * c, -2.f * kFar); }   // a thread far below the row's maximum adds nothing
 __device__ __forceinline__ float delta(float m, float c, float R) { return fmaf(-m, c, R); }   // d from m less d from R
 template <bool NEAR> struct Expo {
   uint64_t a, b;
