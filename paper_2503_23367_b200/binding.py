@@ -406,10 +406,11 @@ def _new2(n: int, m: int, like: torch.Tensor, dtype=_F32) -> torch.Tensor:
 
 
 def _grad_out(logits: torch.Tensor, ld: int, dev: int, out: Optional[torch.Tensor]):
-    """The tensor of a gradient of the logits: given, or new with the logits' row stride (its rows then start at the same offsets from 16 bytes)."""
+    """The tensor of a gradient of the logits: given, or new with rows at the same offsets from 16 bytes as the logits' and no further apart than that takes."""
     rows, V = logits.shape
     if out is None:
-        ld = max(ld, V)
+        per = 16 // logits.element_size()
+        ld = V + max(ld - V, 0) % per
         pad = (logits.data_ptr() & 15) // logits.element_size()
         if pad:
             out = torch.empty_strided((pad + rows * ld,), (1,), dtype=logits.dtype, device=logits.device).as_strided((rows, V), (ld, 1), pad)
