@@ -436,8 +436,10 @@ fv_status fv_generate(fv_ctx *ctx, const fv_generator *gen, const float *start_d
  *   tau         1e-6 ... 1e6.
  *   stats       [rows] pairs (m, L), 8-byte aligned: what the gradient calls take.  ln sum_j exp(x_j / tau) = m / tau + L.
  *   Logits of -inf have p = 0.  A row of nothing but -inf has p = 0 everywhere: m = L = logprob = -inf, entropy 0, gradient 0.
- *   A row that holds a NaN or +inf: every result of it is NaN (m: the largest of the others), its alternatives -1.
- *   A row whose gradient's weights are all 0, or that has no token, has gradient 0 whatever its logits are.
+ *   A row that holds a NaN or +inf: L, entropy, log probabilities, loss and gradients are NaN, its alternatives -1; m passes over NaN and is +inf
+ *   where the row holds one (of nothing but NaN and -inf: -inf).
+ *   Whatever its logits are, a row without a token has log probability 0 and one without a teacher's entries loss 0, and where its weights are 0 as well or have
+ *   nothing to weigh (g_logprob without a token, g_loss without entries), its gradient is 0.
  *   Token ids: -1 stands for none; another id outside [0, V) sets *status_dev (int32 device word, or NULL) to 40, makes the row's
  *   log probability or loss NaN and counts as none in the gradients.
  *   dlogits_out_dev [rows, V] of the type of the logits, rows ld_out elements apart, rounded once from fp32; it may be logits_dev itself (with
@@ -468,7 +470,8 @@ fv_status fv_token_logprobs_grad(const void *logits_dev, int32_t dtype, int64_t 
  * K entries, p over the whole row of logits.
  *   teacher_ids_dev int32, teacher_logits_dev fp32, both [rows, K], K 1 ... 128; log probabilities do as well as logits (the
  *               alternatives of fv_token_logprobs on the teacher's rows).  Entries with id -1 or a logit of -inf are left out; a row
- *               without entries has loss 0.  An id may come more than once; its entries add up.
+ *               without entries has loss 0.  An id may come more than once; its entries add up.  An entry whose logit is NaN or +inf
+ *               makes the row's loss NaN, and its gradient at the tokens of its entries.
  *   loss_out_dev [rows] fp32; stats_out_dev or NULL.
  *   dlogits_out_dev NULL, or the gradient in the same pass: g_loss[r] (p_j - sum_{k: id_k = j} q_k) / tau, g_loss_dev [rows] fp32 or NULL (1);
  *               g_loss_dev is NULL without dlogits_out_dev.
