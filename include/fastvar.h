@@ -468,8 +468,9 @@ fv_status fv_token_logprobs_grad(const void *logits_dev, int32_t dtype, int64_t 
 
 /* Distillation from a teacher's top logits: loss[r] = sum_k q_k (ln q_k - ln p_{id_k}), q = softmax(teacher_logits / tau) over the row's
  * K entries, p over the whole row of logits.
- *   teacher_ids_dev int32, teacher_logits_dev fp32, both [rows, K], K 1 ... 128; log probabilities do as well as logits (the
- *               alternatives of fv_token_logprobs on the teacher's rows).  Entries with id -1 or a logit of -inf are left out; a row
+ *   teacher_ids_dev int32, teacher_logits_dev fp32, both [rows, K], K 1 ... 128; log probabilities of temperature 1 do as well as
+ *               logits (the alternatives of fv_token_logprobs on the teacher's rows; those of another temperature are divided by it already: times it
+ *               they do).  Entries with id -1 or a logit of -inf are left out; a row
  *               without entries has loss 0.  An id may come more than once; its entries add up.  An entry whose logit is NaN or +inf
  *               makes the row's loss NaN, and its gradient at the tokens of its entries.
  *   loss_out_dev [rows] fp32; stats_out_dev or NULL.

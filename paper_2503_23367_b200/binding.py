@@ -462,7 +462,8 @@ def fv_token_logprobs_grad(logits: torch.Tensor, ids: Optional[torch.Tensor], st
 def fv_distill_topk(logits: torch.Tensor, teacher_ids: torch.Tensor, teacher_logits: torch.Tensor, tau: float = 1.0,
                     g_loss: Optional[torch.Tensor] = None, want_grad: bool = False, out: Optional[torch.Tensor] = None,
                     status: Optional[torch.Tensor] = None) -> dict:
-    """Loss per row against a teacher's top logits ([rows, K], ids int32, -1 = no entry): {"loss" [rows], "stats" [rows, 2]} and, with
+    """Loss per row against a teacher's top logits ([rows, K], ids int32, -1 = no entry; alternatives of fv_token_logprobs at temperature t do as
+    t * alt_logprob): {"loss" [rows], "stats" [rows, 2]} and, with
     want_grad, "dlogits" = g_loss[r] * its gradient (g_loss None: 1) from the same pass; out may be the logits themselves."""
     x, dt, ld, rows, V, dev = _rows(logits)
     K = teacher_ids.shape[-1]

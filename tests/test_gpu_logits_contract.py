@@ -1,9 +1,9 @@
-"""What the header promises for rows of logits beyond ordinary ones: rows that hold a NaN or +inf, teachers that do."""
+"""What the header promises for rows of logits beyond ordinary ones: rows that hold a NaN or +inf, teachers that do, alternatives of another temperature as a teacher."""
 import pytest
 import torch
 
 from paper_2503_23367_b200 import binding as fv
-from test_gpu_logits import BF16, DEV, F32, INF, U, near, rows_of
+from test_gpu_logits import BF16, DEV, F32, INF, LN, U, check_distill, near, rows_of
 
 pytestmark = pytest.mark.gpu
 NAN = float("nan")
@@ -75,3 +75,18 @@ def test_a_teacher_with_nan_or_infinity(V, bad):
     assert torch.isnan(d["loss"][1]) and torch.isnan(d["dlogits"][1, [5, 70, 800]]).all() and torch.isnan(late[1, [5, 70, 800]]).all()
     for r in (0, 2):
         assert torch.equal(d["loss"][r], clean["loss"][r]) and torch.equal(d["dlogits"][r], clean["dlogits"][r]) and torch.isfinite(late[r]).all()
+
+
+@pytest.mark.parametrize("tau", [2.0, 0.6])
+def test_alternatives_of_another_temperature_as_a_teacher(tau):
+    """ln p at temperature tau is the logit over tau and a constant of the row, so tau ln p serves as the teacher's logits: what is a multiple of
+    tau apart rounds by 2 u of ln p tau, which the loss divides by tau again."""
+    x, _ = rows_of(200, 5000, F32, 13)
+    teacher, _ = rows_of(200, 5000, F32, 14)
+    alt = fv.fv_token_logprobs(teacher, n_alt=20, tau=tau)
+    raw = teacher.gather(1, alt["alt_ids"].long())
+    a = fv.fv_distill_topk(x, alt["alt_ids"], tau * alt["alt_logprob"], tau=tau)["loss"]
+    b = fv.fv_distill_topk(x, alt["alt_ids"], raw, tau=tau)["loss"]
+    off = 4 * U * (alt["alt_logprob"].abs().amax(1).double() + raw.abs().amax(1).double() / tau) + LN
+    near(a, b, 2 * off * (1 + b.double().abs()))
+    check_distill(x, alt["alt_ids"], (tau * alt["alt_logprob"]).contiguous(), None, tau)
