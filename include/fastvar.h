@@ -492,7 +492,8 @@ fv_status fv_distill_topk_grad(const void *logits_dev, int32_t dtype, int64_t ld
  *   a_dev bf16 [rows, C] (fv_gather_ln's output for the head), w_dev bf16 [V, C], bias_dev bf16 [V] or NULL; C % 8 == 0, V % 8 == 0, all
  *   16-byte aligned, as for fv_gemm_bf16 (W is a constant of the stream).  Products accumulate in fp32, at most 512 of C in one piece; logits
  *   stay fp32.  A bias of -inf forbids a token.  tau, ids and the outputs as for fv_token_logprobs.
- *   workspace_dev: fv_linear_logprobs_workspace_bytes(rows, V) bytes, 256-byte aligned.  Errors: INVALID_ARG, UNSUPPORTED, CAPACITY, CUDA. */
+ *   rows, C and V up to 2^31 - 256 and fewer than 2^31 - 256 tiles of 256 x 128, else UNSUPPORTED.
+ *   workspace_dev: fv_linear_logprobs_workspace_bytes(rows, V) bytes, 256-byte aligned (0 for sizes that are refused).  Errors: INVALID_ARG, UNSUPPORTED, CAPACITY, CUDA. */
 size_t fv_linear_logprobs_workspace_bytes(int32_t rows, int32_t V);
 fv_status fv_linear_logprobs(const void *a_dev, const void *w_dev, const void *bias_dev, int32_t rows, int32_t C, int32_t V,
                              float tau, const int32_t *ids_dev, float *logprob_out_dev, float *stats_out_dev,

@@ -339,6 +339,10 @@ template <int BN> cudaError_t launch_width(const void* a, const void* w, const L
 constexpr int kFewRows = 48, kFewColumns = 9472, kFewK = 2048;
 size_t few_rows_bytes(int rows, int V) { return rows <= kFewRows && V <= kFewColumns ? (size_t)rows * V * 4 : 0; }
 
+// Rows, channels, columns and tiles are counted in 32 bits, a tile or a block of K past the last.
+constexpr int kMostSize = INT_MAX - 255;
+bool too_large(int rows, int V) { return rows > kMostSize || V > kMostSize || (long long)((rows + 255) / 256) * ((V + 127) / 128) > kMostSize; }
+
 bool aligned_to(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 
 }  // namespace
@@ -349,7 +353,7 @@ using namespace fv;
 extern "C" {
 
 size_t fv_linear_logprobs_workspace_bytes(int32_t rows, int32_t V) {
-  if (rows <= 0 || V <= 0) return 0;
+  if (rows <= 0 || V <= 0 || too_large(rows, V)) return 0;
   const size_t parts = align_up((size_t)rows * column_parts(rows, V) * sizeof(float4), 256) + align_up((size_t)rows * 4, 256);
   return std::max(parts, align_up(few_rows_bytes(rows, V), 256));
 }
@@ -360,7 +364,7 @@ fv_status fv_linear_logprobs(const void* a_dev, const void* w_dev, const void* b
   if (!a_dev || !w_dev || rows <= 0 || C <= 0 || (C % 8) || V <= 0 || (V % 8) || !(tau >= 1e-6f && tau <= 1e6f)) return FV_ERR_INVALID_ARG;
   if (!aligned_to(a_dev, 16) || !aligned_to(w_dev, 16) || !aligned_to(bias_dev, 16) || !workspace_dev || !aligned_to(workspace_dev, 256)) return FV_ERR_INVALID_ARG;
   if ((ids_dev != nullptr) != (logprob_out_dev != nullptr) || !aligned_to(stats_out_dev, 8) || (!logprob_out_dev && !stats_out_dev && !entropy_out_dev)) return FV_ERR_INVALID_ARG;
-  if ((long long)((rows + 255) / 256) * ((V + 127) / 128) > INT_MAX) return FV_ERR_UNSUPPORTED;
+  if (C > kMostSize || too_large(rows, V)) return FV_ERR_UNSUPPORTED;
   if (workspace_bytes < fv_linear_logprobs_workspace_bytes(rows, V)) return FV_ERR_CAPACITY;
   if (C <= kFewK && few_rows_bytes(rows, V) > 0) {
     const fv_status s = fv_gemm_bf16(a_dev, w_dev, bias_dev, rows, V, C, EPI_F32, workspace_dev, nullptr, nullptr, 0, rows, status_dev, nullptr, 0, stream);
