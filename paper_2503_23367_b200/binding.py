@@ -465,6 +465,7 @@ def fv_distill_topk(logits: torch.Tensor, teacher_ids: torch.Tensor, teacher_log
     """Loss per row against a teacher's top logits ([rows, K], ids int32, -1 = no entry; alternatives of fv_token_logprobs at temperature t do as
     t * alt_logprob): {"loss" [rows], "stats" [rows, 2]} and, with
     want_grad, "dlogits" = g_loss[r] * its gradient (g_loss None: 1) from the same pass; out may be the logits themselves."""
+    assert out is None or want_grad, "out is the place of the gradient: it goes with want_grad"
     x, dt, ld, rows, V, dev = _rows(logits)
     K = teacher_ids.shape[-1]
     loss, stats = _new(rows, logits), _new2(rows, 2, logits)
