@@ -497,7 +497,9 @@ def _linear_workspace_bytes(rows: int, V: int) -> int:
 
 def fv_linear_logprobs(a: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Tensor], ids: Optional[torch.Tensor] = None, tau: float = 1.0,
                        want_entropy: bool = False, status: Optional[torch.Tensor] = None) -> dict:
-    """As fv_token_logprobs on the rows a [rows, C] * w [V, C]^T + bias [V] (all bf16), whose logits are not kept."""
+    """As fv_token_logprobs on the rows a [rows, C] * w [V, C]^T + bias [V] (all bf16), whose logits are not kept.
+    w is a constant of the stream, as for fv_gemm_bf16: its first tiles are asked for while the calls of this library just before may still run, so it is not what one of those
+    writes (a copy or an event between them puts that right).  What torch has computed on the stream, w.bfloat16() for one, is complete by then.  a, bias and ids may be the product of the call before."""
     rows, Cw = a.shape
     V = w.shape[0]
     dev, bf = a.get_device(), torch.bfloat16
