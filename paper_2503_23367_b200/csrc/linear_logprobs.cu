@@ -66,8 +66,9 @@ template <int N> __device__ __forceinline__ float pick(const float* acc, int i) 
   }
 }
 
-// Bound by the product: 8192 x 2048 -> 4096 97 us, 1.42 PFLOP/s (the plain bf16 GEMM of the shape 92); a round of tiles ends with one epilogue that nothing
-// covers (1.6 us), small calls are the fixed cost of a pair kernel (169 x 1024 -> 4096 9 us with the second launch).
+// Bound by the product: 8192 x 2048 -> 4096 97 us, 1.42 PFLOP/s (the plain bf16 GEMM of the shape 92), the tensor pipe active 78 % of the SMs' time; a round of tiles ends with one epilogue that nothing
+// covers (1.6 us), small calls are the fixed cost of a pair kernel (169 x 1024 -> 4096 9 us with the second launch: 32 tiles on 64 SMs).  320 threads leave 168 registers a thread, of which the 256-wide
+// build spills 68 bytes (128 accumulators); the 128-wide one, 160 registers, none.
 template <int BN>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 linear_logprobs_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const LinearArgs p) {
@@ -253,7 +254,8 @@ linear_logprobs_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
 }
 
 // The row's parts put together.  A CTA has R rows, neighbouring threads neighbouring rows; its 256 / R threads of a row take the parts in turn.  32 rows where there are
-// few parts; 8 where there are many, of which a thread would else read a long chain (300 rows of 512 parts: 24 us beside the product with 32 rows, 4 with 8).
+// few parts; 8 where there are 64 or more, of which a thread would else read a long chain.  us of both launches, 8 rows / 32, C 512: 1000 rows of 2048 (32 parts) 8.8 / 8.2, of 4096 (32) 12.3 / 11.4, of 8192 (64) 16.9 / 18.3, of 16384
+// (128) 25.9 / 29.3; 300 rows of 2048 (32) 7.6 / 7.5, of 4096 (64) 8.3 / 8.6, of 16384 (128) 17.7 / 21.2, of 65536 (512) 42 / 58.
 constexpr int kFinishThreads = 256, kFinishWarps = kFinishThreads / 32, kManyParts = 64;
 struct FinishArgs {
   const float4* part; const float* xid; const int32_t* ids;
@@ -335,7 +337,10 @@ template <int BN> cudaError_t launch_width(const void* a, const void* w, const L
 }
 
 // Few rows: the product with K split over a cluster (fv_gemm_bf16; its slices are at most 512 of K for these sizes, so its sums are as exact) and the rows read back from
-// L2, which is sooner done than 256-row tiles (one row, C 1024, V 4096: 10.8 -> 5.5 us).
+// L2, which is sooner done than 256-row tiles while weights bound both.  us, this route / tiles, 1, 16, 32, 48 rows: C 1024, V 4096 5.6 / 10.9, 6.3 / 9.4, 6.4 / 9.4, 7.7 / 9.5; C 2048, V 4096 7.7 / 18.1,
+// 8.2 / 13.8, 8.2 / 13.4, 9.6 / 13.3; C 2048, V 9472 14.7 / 23.1, 15.2 / 18.8, 15.2 / 15.7, 17.7 / 16.0; C 512, V 9472 9.5 / 10.0, 10.3 / 9.9, 10.8 / 10.3, 12.7 / 10.6: 48 rows of many columns are where it loses.
+// Beyond these limits fv_gemm_bf16 adds more of K in one piece, so that such calls take the tiles although it would be sooner done for some (128 rows, C 2048, V 4096 11.9 / 13.5; one row, C 1024, V 16384 9.5 / 17.2,
+// V 65536 33 / 50; one row, C 4096, V 4096 10.5 / 27.3), with up to five times the error of their logits.
 constexpr int kFewRows = 48, kFewColumns = 9472, kFewK = 2048;
 size_t few_rows_bytes(int rows, int V) { return rows <= kFewRows && V <= kFewColumns ? (size_t)rows * V * 4 : 0; }
 

@@ -587,7 +587,7 @@ template <typename T, bool ENT> __device__ __forceinline__ void tell_row(const T
 
 // One read of the rows.  Counted per 32 logits of rows of 50021: 5.9 warp instructions (bf16; fp32 6.4) with one exponential per logit, 1.6 more with the entropy; and per
 // row, with alternatives, 740 more for a warp's (4096, 8 of them) or 4500 for four warps' (50021, 20 of them).  So long rows are bound by DRAM (4800 x 32768 fp32 93 us, 6.8 TB/s with what L2 held) or, bf16 with entropy and alternatives, by
-// instructions (3001 x 50021, 20 alternatives, 69 us, issue 68 %); many short rows by how many are on their way beside the 6700 clocks behind each one's last logit (8192 x 4096
+// instructions (3001 x 50021, 20 alternatives, 69 us, issue 67 %); many short rows by how many are on their way beside the 6700 clocks behind each one's last logit (8192 x 4096
 // fp32, 8 alternatives, 27 us, 4.9 TB/s); few rows by the chain of steps (two of 4096 with 5 alternatives 4.2 us, four of 131072 with 20 on clusters of eight 6.9).
 template <typename T, int G, bool ENT, bool ALT>
 __global__ void __launch_bounds__(kStreamThreads, 8) token_logprobs_kernel(const TokenArgs p) {
@@ -1142,7 +1142,8 @@ __global__ void __launch_bounds__(32 * kGradWarps) token_logprobs_grad_kernel(co
   }
 }
 
-// As above, and every warp weighs the teacher's entries itself (some 200 instructions beside 600 for its logits: U 8).  2048 x 16384 fp32, K 32: 45 us, 6 TB/s.
+// As above, and every warp weighs the teacher's entries itself (some 200 instructions beside 600 for its logits: U 8) and looks for tokens that come twice, which grows with the square of K / 32: 2048 x 16384 fp32, K 32:
+// 46 us, 5.8 TB/s; K 128: 168.  4096 x 131072 bf16, K 64: 408 us, 5.3 TB/s; K 128: 701.
 template <typename T, int U>
 __global__ void __launch_bounds__(32 * kGradWarps) distill_grad_kernel(const GradArgs p) {
   constexpr int E = Elem<T>::E;
@@ -1242,7 +1243,9 @@ Shape stream_shape(int nv, int rows, int n_alt) {
   const int lg = spread(nv, rows, 0);
   return {128, lg, (nv + (1 << lg) - 1) >> lg};
 }
-// Parts of at most 32 KB, six to an SM: us for 4096 rows of 256 KB, 64 threads to a part of up to 2048 vectors 455, 128 383, 256 568; parts of 64 KB and 256 threads 386.
+// Parts of at most 32 KB, six to an SM, for rows of up to 256 KB: us for 4096 rows of 256 KB, 64 threads to a part of up to 2048 vectors 455, 128 383, 256 568; parts of 64 KB and 256 threads 386.
+// Longer rows stay with eight CTAs, whose parts grow to 192 KB: fewer to an SM.  us, loss and gradient in this one call / in two (fv_distill_topk, then fv_distill_topk_grad) / the bytes of one read and
+// one write: 1024 x 131072 fp32 189 / 265 / 164, 1024 x 200000 fp32 304 / 406 / 251, bf16 199 / 216 / 125, 1024 x 393216 bf16 343 / 417 / 246; at the end of the range 256 x 390000 fp32 244 / 234 / 122.
 Shape kept_shape(int nv, int rows) {
   int lg = 0;
   while ((1 << lg) < kMaxCluster && (nv + (1 << lg) - 1) >> lg > 2048) ++lg;
