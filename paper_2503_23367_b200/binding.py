@@ -397,6 +397,14 @@ def _arg(t: Optional[torch.Tensor], dtype: torch.dtype, shape, dev: int) -> Opti
     return t.data_ptr()
 
 
+def _word(status: Optional[torch.Tensor], dev: int) -> Optional[int]:
+    """Address of the status word: an int32 tensor on that device, a raw address, or None."""
+    if status is None or isinstance(status, int):
+        return status
+    assert status.dtype is _I32 and status.numel() > 0 and status.get_device() == dev, f"status is an int32 word on cuda:{dev}"
+    return status.data_ptr()
+
+
 def _new(n: int, like: torch.Tensor, dtype=_F32) -> torch.Tensor:
     return torch.empty_strided((n,), (1,), dtype=dtype, device=like.device)
 
@@ -441,7 +449,7 @@ def fv_token_logprobs(logits: torch.Tensor, ids: Optional[torch.Tensor] = None, 
         r["alt_ids"] = alt = _new2(rows, n_alt, logits, _I32)
         r["alt_logprob"] = altl = _new2(rows, n_alt, logits)
         altp, altlp = alt.data_ptr(), altl.data_ptr()
-    _check(lib().fv_token_logprobs(x, dt, ld, rows, V, tau, idp, n_alt, lpp, stats.data_ptr(), entp, altp, altlp, _ptr(status), _stream()),
+    _check(lib().fv_token_logprobs(x, dt, ld, rows, V, tau, idp, n_alt, lpp, stats.data_ptr(), entp, altp, altlp, _word(status, dev), _stream()),
            "fv_token_logprobs")
     return r
 
@@ -454,7 +462,7 @@ def fv_token_logprobs_grad(logits: torch.Tensor, ids: Optional[torch.Tensor], st
     out, op, ldo = _grad_out(logits, ld, dev, out)
     one = (rows,)
     _check(lib().fv_token_logprobs_grad(x, dt, ld, rows, V, tau, _arg(ids, _I32, one, dev), _arg(stats, _F32, (rows, 2), dev), _arg(entropy, _F32, one, dev),
-                                        _arg(g_logprob, _F32, one, dev), _arg(g_entropy, _F32, one, dev), op, ldo, _ptr(status), _stream()),
+                                        _arg(g_logprob, _F32, one, dev), _arg(g_entropy, _F32, one, dev), op, ldo, _word(status, dev), _stream()),
            "fv_token_logprobs_grad")
     return out
 
@@ -474,7 +482,7 @@ def fv_distill_topk(logits: torch.Tensor, teacher_ids: torch.Tensor, teacher_log
     if want_grad:
         r["dlogits"], op, ldo = _grad_out(logits, ld, dev, out)
     _check(lib().fv_distill_topk(x, dt, ld, rows, V, tau, _arg(teacher_ids, _I32, (rows, K), dev), _arg(teacher_logits, _F32, (rows, K), dev), K,
-                                 _arg(g_loss, _F32, (rows,), dev), loss.data_ptr(), stats.data_ptr(), op, ldo, _ptr(status), _stream()), "fv_distill_topk")
+                                 _arg(g_loss, _F32, (rows,), dev), loss.data_ptr(), stats.data_ptr(), op, ldo, _word(status, dev), _stream()), "fv_distill_topk")
     return r
 
 
@@ -486,7 +494,7 @@ def fv_distill_topk_grad(logits: torch.Tensor, teacher_ids: torch.Tensor, teache
     K = teacher_ids.shape[-1]
     out, op, ldo = _grad_out(logits, ld, dev, out)
     _check(lib().fv_distill_topk_grad(x, dt, ld, rows, V, tau, _arg(teacher_ids, _I32, (rows, K), dev), _arg(teacher_logits, _F32, (rows, K), dev), K,
-                                      _arg(stats, _F32, (rows, 2), dev), _arg(g_loss, _F32, (rows,), dev), op, ldo, _ptr(status), _stream()), "fv_distill_topk_grad")
+                                      _arg(stats, _F32, (rows, 2), dev), _arg(g_loss, _F32, (rows,), dev), op, ldo, _word(status, dev), _stream()), "fv_distill_topk_grad")
     return out
 
 
@@ -516,7 +524,7 @@ def fv_linear_logprobs(a: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Te
     if want_entropy:
         r["entropy"] = ent = _new(rows, a)
         entp = ent.data_ptr()
-    _check(lib().fv_linear_logprobs(ap, wp, bp, rows, Cw, V, tau, idp, lpp, stats.data_ptr(), entp, (ws.data_ptr() + 255) // 256 * 256, ws_bytes, _ptr(status), _stream()),
+    _check(lib().fv_linear_logprobs(ap, wp, bp, rows, Cw, V, tau, idp, lpp, stats.data_ptr(), entp, (ws.data_ptr() + 255) // 256 * 256, ws_bytes, _word(status, dev), _stream()),
            "fv_linear_logprobs")
     return r
 
