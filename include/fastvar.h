@@ -435,6 +435,7 @@ fv_status fv_generate(fv_ctx *ctx, const fv_generator *gen, const float *start_d
  *               address of their type and V may be odd.  V * (size of an element) <= 1.5 MiB, else UNSUPPORTED.
  *   tau         1e-6 ... 1e6.
  *   stats       [rows] pairs (m, L), 8-byte aligned: what the gradient calls take.  ln sum_j exp(x_j / tau) = m / tau + L.
+ *   A log probability beyond the range of fp32 (the type's lowest logit at tau < 1) is -inf, the loss of an entry of weight q > 0 over it +inf; its p is 0.
  *   Logits of -inf have p = 0.  A row of nothing but -inf has p = 0 everywhere: m = L = logprob = -inf, entropy 0, gradient 0.
  *   A row that holds a NaN or +inf: L, entropy, log probabilities, loss and gradients are NaN, its alternatives -1; m passes over NaN and is +inf
  *   where the row holds one (of nothing but NaN and -inf: -inf).

@@ -90,3 +90,23 @@ def test_alternatives_of_another_temperature_as_a_teacher(tau):
     off = 4 * U * (alt["alt_logprob"].abs().amax(1).double() + raw.abs().amax(1).double() / tau) + LN
     near(a, b, 2 * off * (1 + b.double().abs()))
     check_distill(x, alt["alt_ids"], (tau * alt["alt_logprob"]).contiguous(), None, tau)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("V", [900, 40000])
+def test_log_probabilities_beyond_the_range_of_fp32(V, dtype):
+    """The lowest logit over a temperature of 0.5: -inf, the loss over it +inf however little it weighs, gradients finite."""
+    x, _ = rows_of(3, V, dtype, 15)
+    x[1, 7] = torch.finfo(dtype).min
+    ids = torch.full((3,), 7, dtype=torch.int32, device=DEV)
+    r = fv.fv_token_logprobs(x, ids, tau=0.5, want_entropy=True)
+    assert float(r["logprob"][1]) == -INF and torch.isfinite(r["logprob"][[0, 2]]).all() and torch.isfinite(r["entropy"]).all()
+    t_ids = torch.tensor([[7, 3]] * 3, dtype=torch.int32, device=DEV)
+    t_logits = torch.tensor([[0.0, 2.0]] * 3, device=DEV)
+    for grad in (False, True):
+        d = fv.fv_distill_topk(x, t_ids, t_logits, tau=0.5, want_grad=grad)
+        assert float(d["loss"][1]) == INF and torch.isfinite(d["loss"][[0, 2]]).all()
+    late = fv.fv_distill_topk_grad(x, t_ids, t_logits, d["stats"], tau=0.5)
+    one = torch.ones(3, device=DEV)
+    token = fv.fv_token_logprobs_grad(x, ids, r["stats"], one, tau=0.5, entropy=r["entropy"], g_entropy=one)
+    assert all(torch.isfinite(t.float()).all() for t in (d["dlogits"], late, token))
